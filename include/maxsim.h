@@ -54,7 +54,7 @@ extern "C" {
 #define MAXSIM_ERR_INVALID (-1)     /* null pointer, non-positive size, misaligned pointer, bad enum */
 #define MAXSIM_ERR_UNSUPPORTED (-2) /* an embedding width or a size that the kernels are not built for */
 #define MAXSIM_ERR_LAUNCH (-3)      /* the HIP runtime reported an error at launch */
-#define MAXSIM_ERR_SCRATCH (-4)     /* sizes beyond the library's static scratch buffer (maxsim_backward_csr_static) */
+#define MAXSIM_ERR_SCRATCH (-4)     /* sizes beyond the library's static scratch buffer (maxsim_backward_csr_static) or a workspace */
 
 typedef enum { MAXSIM_F32 = 0, MAXSIM_F16 = 1, MAXSIM_BF16 = 2 } maxsim_dtype;
 
@@ -252,6 +252,87 @@ int maxsim_forward_i8_streamed(const int8_t *Q_i8, const float *q_scale, int n_q
  */
 int maxsim_ce_grad(const float *scores, int n, int b, float tau, float *g, float *loss,
                    void *stream);
+
+/*
+ * Operators of the model that makes the embeddings: rotary positions, attention over packed sequences with its
+ * gradient, and the clipping of gradients by their global norm.  The sequences are laid out as the packed corpus
+ * of maxsim_forward_ragged is: token rows back to back, with int32 offsets on the device.
+ *
+ * Packed tensors [tokens, heads, d] of these entry points may be views (slices of a fused projection, transposed
+ * heads): strides are counted in elements, the innermost one is 1.
+ */
+
+/*
+ * Rotary positions.  For token t at position p(t), and i = 0 .. rot / 2 - 1, the pair (x_i, x_j) of every head becomes
+ *     y_i = scale (x_i cos a - x_j sin a),  y_j = scale (x_i sin a + x_j cos a),  a = p(t) * freqs[i],
+ * with j = i + rot / 2 or, with `neighbours`, the pair (2 i, 2 i + 1).  Entries from rot on are copied.  With
+ * `inverse` the angle's sign is turned: the transposed map, hence the gradient of the forward one.
+ *   X, Y       [tokens, heads, d] dtype    Y may be X (and is otherwise apart from it)
+ *   freqs      [rot / 2] float32           angle per position; 2 <= rot <= d, even, rot <= 4096
+ *   positions  [tokens] int32 or NULL      p(t); NULL: the place of t in its sequence
+ *   offsets    [b + 1] int32 or NULL       the sequences (not looked at where positions are given); NULL: one sequence
+ *   scale      the factor that long-context scalings apply beside their frequencies, 1 otherwise
+ * Angles are reduced in 64 bits, the rotation is computed in fp32 and rounded once.  Rows whose addresses and strides are
+ * multiples of 16 bytes are moved in such pieces; others are taken entry by entry.
+ */
+int maxsim_rope(const void *X, int64_t tokens, int heads, int d, int64_t x_token_stride, int64_t x_head_stride,
+                maxsim_dtype dtype, const float *freqs, int rot, const int32_t *positions, const int32_t *offsets,
+                int64_t b, float scale, int neighbours, int inverse, void *Y, int64_t y_token_stride,
+                int64_t y_head_stride, void *stream);
+
+/*
+ * Attention over b packed sequences: of sequence i, queries q_offsets[i] .. q_offsets[i + 1] see keys
+ * k_offsets[i] .. k_offsets[i + 1] (the same offsets for a whole prompt; few queries against many kept keys and
+ * values when serving).
+ *     O = softmax(scale Q K^T + mask) V,   lse = log sum exp of the masked scores
+ *   Q, O  [q_tokens, hq, d],  K, V [k_tokens, hkv, d]   fp16 or bf16; query head h reads key head h / (hq / hkv)
+ *   strides  HOST int64 [8]: token and head stride of Q, K, V, O in this order, multiples of 8 and token strides below
+ *         2^24; NULL: all without gaps.  Base pointers are multiples of 16 bytes.
+ *   q_offsets, k_offsets [b + 1] int32 (device), as doc_offsets in maxsim_forward_ragged; sequences may be empty
+ *   hq    a multiple of hkv;  d  a multiple of 8 up to 128;  scale > 0
+ *   causal  nonzero: the last query sees all keys, the one before it all but the last, and so on
+ *           (query t of lq sees keys j <= t + lk - lq).  Zero: all queries see all keys of their sequence.
+ *   lse   [q_tokens, hq] float32 or NULL
+ *   workspace  maxsim_attention_workspace(...) bytes (device, 16-byte aligned); may be NULL where that is 0
+ * A query that sees no key gets O = 0 and lse = -inf.  Scores, the softmax's maximum and sum and the sums over keys are
+ * fp32; probabilities are rounded to the inputs' type before they multiply V.  The result is the same on every
+ * run.  What a sequence's rows hold does not reach another sequence's results.
+ */
+int64_t maxsim_attention_workspace(int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, int hkv, int d);
+int maxsim_attention(const void *Q, const void *K, const void *V, const int64_t *strides, const int32_t *q_offsets,
+                     const int32_t *k_offsets, int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, int hkv, int d,
+                     maxsim_dtype dtype, int causal, float scale, void *O, float *lse, void *workspace,
+                     int64_t workspace_bytes, void *stream);
+
+/*
+ * Gradient of maxsim_attention: with P the probabilities and delta = sum_d dO O,
+ *     dV = P^T dO,   dS = P (dO V^T - delta),   dQ = scale dS K,   dK = scale dS^T Q  (summed over a key head's queries)
+ *   O, lse  as maxsim_attention left them;  dO [q_tokens, hq, d] the upstream gradient
+ *   dQ [q_tokens, hq, d], dK, dV [k_tokens, hkv, d]  in the inputs' type, every row fully overwritten (zeros where there is nothing)
+ *   strides  HOST int64 [16]: token and head stride of Q, K, V, O, dO, dQ, dK, dV, as above; NULL: all without gaps
+ *   workspace  maxsim_attention_backward_workspace(...) bytes (device, 16-byte aligned)
+ * Sums are fp32 in a fixed order (no atomics): the same bits on every run.  P and dS are rounded to the inputs' type
+ * before they enter the last products.
+ */
+int64_t maxsim_attention_backward_workspace(int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, int hkv, int d);
+int maxsim_attention_backward(const void *Q, const void *K, const void *V, const void *O, const float *lse,
+                              const void *dO, const int64_t *strides, const int32_t *q_offsets,
+                              const int32_t *k_offsets, int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, int hkv,
+                              int d, maxsim_dtype dtype, int causal, float scale, void *dQ, void *dK, void *dV,
+                              void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * Clipping by the global norm:  norm = sqrt(sum of all gradients' squares),  out_i = min(1, max_norm / (norm + 1e-6)) g_i.
+ *   grads, out  HOST arrays of n device pointers (out[i] may be grads[i]: in place); tensors without gaps, aligned to their elements
+ *   numel       HOST int64 [n], may be 0;  dtypes  HOST int32 [n], maxsim_dtype of grads[i] and out[i]
+ *   norm        [1] float32 (device)
+ *   workspace   maxsim_clip_workspace(n) bytes (device, 16-byte aligned)
+ * The arrays on the host may be reused when the call returns.  Squares are added in fp64 in a fixed order.  A gradient that
+ * is not finite shows in the norm and, as in the formula, in every product with the factor 0 or NaN that it makes.
+ */
+int64_t maxsim_clip_workspace(int n);
+int maxsim_clip_grad_norm(const void *const *grads, void *const *out, const int64_t *numel, const int32_t *dtypes,
+                          int n, float max_norm, float *norm, void *workspace, int64_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

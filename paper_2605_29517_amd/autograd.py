@@ -40,3 +40,50 @@ def maxsim(Q, D, doc_offsets=None):
     if doc_offsets is None:
         return _MaxSim.apply(Q, D)
     return _MaxSimRagged.apply(Q, D, doc_offsets)
+
+
+def _rows(t):
+    """t as the attention and rotary entry points take it: rows of stride 1 in pieces of 16 bytes (a view if it is one of those)."""
+    size = t.element_size()
+    fine = t.dim() == 3 and t.stride(2) == 1 and (t.data_ptr() | t.stride(0) * size | t.stride(1) * size) % 16 == 0
+    return t if fine else t.contiguous()
+
+
+class _Rope(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, X, freqs, positions, offsets, interleaved, scale):
+        ctx.save_for_backward(freqs, positions, offsets)
+        ctx.how = interleaved, scale
+        return M.maxsim_rope(_rows(X), freqs, positions, offsets, interleaved=interleaved, scale=scale)
+
+    @staticmethod
+    def backward(ctx, dY):
+        freqs, positions, offsets = ctx.saved_tensors
+        interleaved, scale = ctx.how
+        return M.maxsim_rope(_rows(dY), freqs, positions, offsets, interleaved=interleaved, scale=scale, inverse=True), None, None, None, None, None
+
+
+class _Attention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, Q, K, V, q_offsets, k_offsets, causal, scale):
+        Q, K, V = _rows(Q), _rows(K), _rows(V)
+        out, lse = M.maxsim_attention(Q, K, V, q_offsets, k_offsets, causal=causal, scale=scale)
+        ctx.save_for_backward(Q, K, V, out, lse, q_offsets, k_offsets)
+        ctx.how = causal, scale
+        return out
+
+    @staticmethod
+    def backward(ctx, dout):
+        Q, K, V, out, lse, q_offsets, k_offsets = ctx.saved_tensors
+        causal, scale = ctx.how
+        return M.maxsim_attention_backward(Q, K, V, out, lse, _rows(dout), q_offsets, k_offsets, causal=causal, scale=scale) + (None,) * 4
+
+
+def rope(X, freqs, positions=None, offsets=None, interleaved=False, scale=1.0):
+    """Differentiable rotary positions of X [tokens, heads, d] (binding.maxsim_rope; no gradient for freqs)."""
+    return _Rope.apply(X, freqs, positions, offsets, interleaved, scale)
+
+
+def attention(Q, K, V, q_offsets, k_offsets=None, causal=True, scale=None):
+    """Differentiable attention over packed sequences (binding.maxsim_attention)."""
+    return _Attention.apply(Q, K, V, q_offsets, k_offsets, causal, scale)

@@ -21,7 +21,9 @@ _DTYPE = {torch.float32: MAXSIM_F32, torch.float16: MAXSIM_F16, torch.bfloat16: 
 
 SYMBOLS = ("maxsim_strerror", "maxsim_init", "maxsim_forward", "maxsim_forward_ragged", "maxsim_forward_streamed", "maxsim_backward", "maxsim_backward_ragged",
            "maxsim_csr_build", "maxsim_backward_csr", "maxsim_backward_csr_static",
-           "maxsim_quantize_rows_i8", "maxsim_forward_i8", "maxsim_forward_i8_ragged", "maxsim_forward_i8_streamed", "maxsim_ce_grad")
+           "maxsim_quantize_rows_i8", "maxsim_forward_i8", "maxsim_forward_i8_ragged", "maxsim_forward_i8_streamed", "maxsim_ce_grad",
+           "maxsim_rope", "maxsim_attention_workspace", "maxsim_attention", "maxsim_attention_backward_workspace", "maxsim_attention_backward",
+           "maxsim_clip_workspace", "maxsim_clip_grad_norm")
 
 _lib = None
 # The native part (csrc/marshal.cpp) of the functions that a latency-bound program calls: the checks below, the outputs, the stream
@@ -73,6 +75,19 @@ def load():
     L.maxsim_forward_i8_streamed.argtypes = [p, p, i, i, p, p, l, i, i, l, p, p, p, p]
     L.maxsim_ce_grad.restype = i
     L.maxsim_ce_grad.argtypes = [p, i, i, f, p, p, p]
+    L.maxsim_rope.restype = i
+    L.maxsim_rope.argtypes = [p, l, i, i, l, l, i, p, i, p, p, l, f, i, i, p, l, l, p]
+    for name in ("maxsim_attention_workspace", "maxsim_attention_backward_workspace"):
+        getattr(L, name).restype = l
+        getattr(L, name).argtypes = [l, l, l, i, i, i]
+    L.maxsim_attention.restype = i
+    L.maxsim_attention.argtypes = [p, p, p, p, p, p, l, l, l, i, i, i, i, i, f, p, p, p, l, p]
+    L.maxsim_attention_backward.restype = i
+    L.maxsim_attention_backward.argtypes = [p, p, p, p, p, p, p, p, p, l, l, l, i, i, i, i, i, f, p, p, p, p, l, p]
+    L.maxsim_clip_workspace.restype = l
+    L.maxsim_clip_workspace.argtypes = [i]
+    L.maxsim_clip_grad_norm.restype = i
+    L.maxsim_clip_grad_norm.argtypes = [p, p, p, p, i, f, p, p, l, p]
     L.maxsim_init.restype = i
     L.maxsim_init.argtypes = []
     native = _load_native()
@@ -505,3 +520,141 @@ def maxsim_ce_grad(scores, tau, g=None, loss=None):
                               _dev(loss, "loss", torch.float32), _stream(scores))
     _check(rc, "maxsim_ce_grad")
     return g, loss
+
+
+def _rows(t: torch.Tensor, name: str, shape=None, dtype=None):
+    """Token and head stride of a packed tensor [tokens, heads, d], which may be a view: rows of d entries that lie together."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise MaxSimError("%s must be a tensor on the GPU" % name)
+    if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise MaxSimError("%s must be [tokens, heads, d] with rows of stride 1" % name)
+    if shape is not None:
+        _same(t, name, shape, dtype)
+    d = t.shape[2]  # (the stride of a dimension of one entry is not looked at by anybody)
+    return (t.stride(0) if t.shape[0] > 1 else d, t.stride(1) if t.shape[1] > 1 else d)
+
+
+def maxsim_rope(X, freqs, positions=None, offsets=None, interleaved=False, inverse=False, scale=1.0, out=None):
+    """Rotary positions of X [tokens, heads, d] (a view may be given: queries and keys of one projection turn in one call): the first
+    2 * len(freqs) entries of each head turn by position * freqs, in halves (i, i + rot / 2) or neighbours (interleaved).  Positions are
+    given (int32 [tokens]), or a token's place in its sequence (offsets int32 [b + 1]), or its row.  inverse: the gradient's
+    direction.  out may be X."""
+    L = load()
+    xt, xh = _rows(X, "X")
+    T, H, d = X.shape
+    if X.dtype not in _DTYPE:
+        raise MaxSimError("X must have a dtype in {fp32, fp16, bf16}")
+    if out is None:
+        out = torch.empty(T, H, d, dtype=X.dtype, device=X.device)
+    yt, yh = _rows(out, "out", (T, H, d), X.dtype)
+    if freqs.dim() != 1 or not 2 <= 2 * freqs.shape[0] <= d:
+        raise MaxSimError("freqs must be [rot / 2] with rot at most %d" % d)
+    if positions is not None:
+        _same(positions, "positions", (T,))
+        offsets = None
+    if offsets is not None and (offsets.dim() != 1 or offsets.shape[0] < 2):
+        raise MaxSimError("offsets must hold b + 1 >= 2 entries")
+    _same_device(X, freqs=freqs, positions=positions, offsets=offsets, out=out)
+    with torch.cuda.device(X.device):
+        rc = L.maxsim_rope(X.data_ptr(), T, H, d, xt, xh, _DTYPE[X.dtype], _dev(freqs, "freqs", torch.float32), 2 * freqs.shape[0],
+                           _dev(positions, "positions", torch.int32) if positions is not None else None,
+                           _dev(offsets, "offsets", torch.int32) if offsets is not None else None, offsets.shape[0] - 1 if offsets is not None else 0,
+                           float(scale), int(bool(interleaved)), int(bool(inverse)), out.data_ptr(), yt, yh, _stream(X))
+    _check(rc, "maxsim_rope")
+    return out
+
+
+def _attention_sizes(Q, K, V, q_offsets, k_offsets, scale):
+    """Strides of Q, K, V, the offsets and the sizes that the C side takes."""
+    strides = _rows(Q, "Q") + _rows(K, "K") + _rows(V, "V")
+    (tq, hq, d), (tk, hkv, _) = Q.shape, K.shape
+    if k_offsets is None:
+        k_offsets = q_offsets
+    if K.shape[2] != d or K.shape != V.shape or hkv < 1 or hq % hkv != 0:
+        raise MaxSimError("K and V must be [k_tokens, hkv, d] with Q's d and a number of heads that divides Q's")
+    if Q.dtype not in (torch.float16, torch.bfloat16) or K.dtype != Q.dtype or V.dtype != Q.dtype:
+        raise MaxSimError("Q, K and V must share a dtype in {fp16, bf16}")
+    if q_offsets.dim() != 1 or q_offsets.shape != k_offsets.shape or q_offsets.shape[0] < 2:
+        raise MaxSimError("q_offsets and k_offsets must both hold b + 1 >= 2 entries")
+    if k_offsets is q_offsets and tq != tk:
+        raise MaxSimError("Q and K must have the same rows where they share their offsets")
+    return strides, q_offsets, k_offsets, (q_offsets.shape[0] - 1, tq, tk, hq, hkv, d), d ** -0.5 if scale is None else float(scale)
+
+
+def _workspace(given, needed, like):
+    if given is None:
+        return torch.empty(needed, dtype=torch.uint8, device=like.device) if needed else None
+    _dev(given, "workspace", torch.uint8)
+    _same_device(like, workspace=given)
+    return given
+
+
+def maxsim_attention(Q, K, V, q_offsets, k_offsets=None, causal=True, scale=None, out=None, lse=None, workspace=None):
+    """Attention over packed sequences: Q [q_tokens, hq, d], K and V [k_tokens, hkv, d] (fp16 or bf16; views may be given), int32 offsets
+    [b + 1] (k_offsets: q_offsets where the same tokens are queries and keys) -> (O like Q, lse fp32 [q_tokens, hq]).  scale: 1 / sqrt(d)
+    where it is not given."""
+    L = load()
+    strides, q_offsets, k_offsets, sizes, scale = _attention_sizes(Q, K, V, q_offsets, k_offsets, scale)
+    if out is None:
+        out = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+    if lse is None:
+        lse = torch.empty(Q.shape[:2], dtype=torch.float32, device=Q.device)
+    strides += _rows(out, "out", Q.shape, Q.dtype)
+    _same(lse, "lse", Q.shape[:2], torch.float32)
+    _same_device(Q, K=K, V=V, q_offsets=q_offsets, k_offsets=k_offsets, out=out, lse=lse)
+    with torch.cuda.device(Q.device):
+        ws = _workspace(workspace, L.maxsim_attention_workspace(*sizes), Q)
+        rc = L.maxsim_attention(Q.data_ptr(), K.data_ptr(), V.data_ptr(), (ctypes.c_int64 * 8)(*strides), _dev(q_offsets, "q_offsets", torch.int32),
+                                _dev(k_offsets, "k_offsets", torch.int32), *sizes, _DTYPE[Q.dtype], int(bool(causal)), scale, out.data_ptr(), _dev(lse, "lse"),
+                                ws.data_ptr() if ws is not None else None, ws.numel() if ws is not None else 0, _stream(Q))
+    _check(rc, "maxsim_attention")
+    return out, lse
+
+
+def maxsim_attention_backward(Q, K, V, out, lse, dout, q_offsets, k_offsets=None, causal=True, scale=None, dQ=None, dK=None, dV=None, workspace=None):
+    """The gradient of maxsim_attention (out and lse as it left them) -> (dQ, dK, dV) in the inputs' type."""
+    L = load()
+    strides, q_offsets, k_offsets, sizes, scale = _attention_sizes(Q, K, V, q_offsets, k_offsets, scale)
+    dQ, dK, dV = (torch.empty(x.shape, dtype=x.dtype, device=x.device) if g is None else g for g, x in ((dQ, Q), (dK, K), (dV, V)))
+    strides += _rows(out, "out", Q.shape, Q.dtype) + _rows(dout, "dout", Q.shape, Q.dtype)
+    strides += _rows(dQ, "dQ", Q.shape, Q.dtype) + _rows(dK, "dK", K.shape, Q.dtype) + _rows(dV, "dV", K.shape, Q.dtype)
+    _same(lse, "lse", Q.shape[:2], torch.float32)
+    _same_device(Q, K=K, V=V, out=out, lse=lse, dout=dout, q_offsets=q_offsets, k_offsets=k_offsets, dQ=dQ, dK=dK, dV=dV)
+    with torch.cuda.device(Q.device):
+        ws = _workspace(workspace, L.maxsim_attention_backward_workspace(*sizes), Q)
+        rc = L.maxsim_attention_backward(Q.data_ptr(), K.data_ptr(), V.data_ptr(), out.data_ptr(), _dev(lse, "lse"), dout.data_ptr(), (ctypes.c_int64 * 16)(*strides),
+                                         _dev(q_offsets, "q_offsets", torch.int32), _dev(k_offsets, "k_offsets", torch.int32), *sizes, _DTYPE[Q.dtype], int(bool(causal)),
+                                         scale, dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), ws.data_ptr() if ws is not None else None,
+                                         ws.numel() if ws is not None else 0, _stream(Q))
+    _check(rc, "maxsim_attention_backward")
+    return dQ, dK, dV
+
+
+def maxsim_clip_grad_norm(grads, max_norm, out=None, norm=None, workspace=None):
+    """Scales gradients (a sequence of tensors, fp32, fp16 or bf16, mixed) by min(1, max_norm / (norm + 1e-6)), norm the 2-norm over all of
+    them: in place, or into the tensors of out.  Returns the norm (fp32 [1], on the GPU: nothing waits for it)."""
+    L = load()
+    grads = list(grads)
+    out = grads if out is None else list(out)
+    if not grads or len(out) != len(grads):
+        raise MaxSimError("grads must hold a tensor at least, and out as many")
+    n = len(grads)
+    for g, o in zip(grads, out):
+        _dev(g, "a gradient")
+        if g.dtype not in _DTYPE:
+            raise MaxSimError("gradients must have a dtype in {fp32, fp16, bf16}")
+        if o is not g:
+            _same(o, "out", g.shape, g.dtype)
+            _dev(o, "out")
+        _same_device(grads[0], gradient=g, out=o)
+    if norm is None:
+        norm = torch.empty(1, dtype=torch.float32, device=grads[0].device)
+    _same(norm, "norm", (1,), torch.float32)
+    _same_device(grads[0], norm=norm)
+    with torch.cuda.device(grads[0].device):
+        ws = _workspace(workspace, L.maxsim_clip_workspace(n), norm)
+        rc = L.maxsim_clip_grad_norm((ctypes.c_void_p * n)(*(g.data_ptr() for g in grads)), (ctypes.c_void_p * n)(*(o.data_ptr() for o in out)),
+                                     (ctypes.c_int64 * n)(*(g.numel() for g in grads)), (ctypes.c_int32 * n)(*(_DTYPE[g.dtype] for g in grads)), n,
+                                     float(max_norm), _dev(norm, "norm"), ws.data_ptr(), ws.numel(), _stream(norm))
+    _check(rc, "maxsim_clip_grad_norm")
+    return norm

@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmaxsim.so")
 PROBE_LIB = os.path.join(HERE, "libmaxsim_probe.so")
 MARSHAL = os.path.join(HERE, "_marshal.so")
-SOURCES = ["api.hip", "forward.hip", "forward_f16.hip", "forward_bf16.hip", "forward_f32.hip", "forward_argmax.hip", "forward_wide.hip", "forward_wide_f16.hip", "forward_wide_bf16.hip", "forward_wide_f32.hip", "forward_splitd.hip", "backward.hip", "int8.hip", "int8_rows64.hip", "int8_wide.hip"]
+SOURCES = ["api.hip", "forward.hip", "forward_f16.hip", "forward_bf16.hip", "forward_f32.hip", "forward_argmax.hip", "forward_wide.hip", "forward_wide_f16.hip", "forward_wide_bf16.hip", "forward_wide_f32.hip", "forward_splitd.hip", "backward.hip", "int8.hip", "int8_rows64.hip", "int8_wide.hip", "rope.hip", "attention.hip", "attention_backward.hip", "clip.hip"]
 PROBE_SOURCES = ["probe.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # packed fp32 VALU forms are switched off on purpose (they have produced wrong results on
@@ -21,7 +21,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
          # inputs are finite by contract: without this every max is preceded by a NaN-quieting copy
          "-fno-honor-nans",
          "-Wall", "-Wno-unused-function"]
-FILE_FLAGS = {"forward_argmax.hip": ["-falign-loops=64"]}  # (the reason is at its top)
+FILE_FLAGS = {"forward_argmax.hip": ["-falign-loops=64"], "clip.hip": ["-fhonor-nans"]}  # (the reasons are at their tops)
 
 
 def marshal_abi():

@@ -3,7 +3,7 @@
 
 #include <mutex>
 
-#include "common.h"
+#include "attention.h"
 
 namespace maxsim {
 hipError_t forward_launch(FwdParams p, int dtype, int d, int num_cu, hipStream_t stream);
@@ -30,6 +30,16 @@ hipError_t forward_i8_launch(const int8_t *Q, const float *qs, int n_q, int l_q,
                              const int32_t *offsets, int64_t b, int l_d, int64_t total_tokens, float *scores,
                              int64_t ld, int num_cu, hipStream_t stream);
 hipError_t ce_grad_launch(const float *scores, int n, int b, float tau, float *g, float *loss, hipStream_t stream);
+bool rope_width_ok(int rot);
+hipError_t rope_launch(const void *X, int64_t tokens, int heads, int d, int64_t x_token, int64_t x_head, int dtype, const float *freqs, int rot,
+                       const int32_t *positions, const int32_t *offsets, int64_t b, float scale, bool neighbours, bool inverse, void *Y, int64_t y_token, int64_t y_head,
+                       hipStream_t stream);
+int64_t attention_workspace(int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, int hkv, int d, int num_cu);
+hipError_t attention_launch(AttnParams p, int dtype, void *workspace, int num_cu, hipStream_t stream);
+int64_t attention_backward_workspace(int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, int hkv, int d, int num_cu);
+hipError_t attention_backward_launch(AttnParams p, int dtype, void *workspace, int num_cu, hipStream_t stream);
+int64_t clip_workspace(int n);
+hipError_t clip_launch(const void *const *g, void *const *out, const int64_t *numel, const int32_t *dtype, int n, float max_norm, float *norm, void *workspace, hipStream_t stream);
 hipError_t forward_splitd_init_device();
 hipError_t forward_wide_init_device();
 hipError_t forward_i8_init_device();
@@ -120,6 +130,64 @@ hipStream_t copy_stream()
         cached[dev] = st;
     }
     return cached[dev];
+}
+
+// Attention: sizes, then pointers and strides of the packed tensors
+int attention_sizes_ok(int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, int hkv, int d)
+{
+    if (b < 1 || q_tokens < 1 || k_tokens < 1 || hq < 1 || hkv < 1 || hq % hkv != 0 || d < 1)
+        return MAXSIM_ERR_INVALID;
+    if (d % 8 != 0 || d > 128 || hq > (1 << 16))
+        return MAXSIM_ERR_UNSUPPORTED;
+    // tiles and rows are counted in int32: (tokens / 32 + sequences) tiles of every head, tokens * heads rows of a sequence
+    const int64_t most = int64_t(1) << 31;
+    if (q_tokens >= most || k_tokens >= most || b >= most || (q_tokens / 32 + k_tokens / 32 + 2 * b) * hq >= (int64_t(1) << 25))
+        return MAXSIM_ERR_UNSUPPORTED;
+    return MAXSIM_OK;
+}
+
+struct AttnTensor {
+    maxsim::AttnRows *to;
+    const void *p;
+    int heads;
+    bool written;
+};
+
+int attention_common(maxsim::AttnParams &p, const AttnTensor *t, int n, const int64_t *strides, const int32_t *q_offsets, const int32_t *k_offsets, int64_t b, int64_t q_tokens,
+                     int64_t k_tokens, int hq, int hkv, int d, int dtype, int causal, float scale, const void *workspace, int64_t workspace_bytes, int64_t needed)
+{
+    if (int rc = attention_sizes_ok(b, q_tokens, k_tokens, hq, hkv, d))
+        return rc;
+    if (!q_offsets || !k_offsets || !aligned(q_offsets, 4) || !aligned(k_offsets, 4) || !dtype_ok(dtype) || !(scale > 0.0f) || !(scale < 1e30f))
+        return MAXSIM_ERR_INVALID;
+    if (dtype == MAXSIM_F32)
+        return MAXSIM_ERR_UNSUPPORTED;
+    for (int i = 0; i < n; ++i) {
+        const int64_t token = strides ? strides[2 * i] : (int64_t)t[i].heads * d, head = strides ? strides[2 * i + 1] : d;
+        if (!t[i].p || !aligned(t[i].p, 16) || token < 0 || head < 0 || token % 8 != 0 || head % 8 != 0)
+            return MAXSIM_ERR_INVALID;
+        if (t[i].written && (token < d || head < d)) // rows of an output lie apart
+            return MAXSIM_ERR_INVALID;
+        if (token >= (1 << 24) || head >= (int64_t(1) << 40))
+            return MAXSIM_ERR_UNSUPPORTED;
+        *t[i].to = {static_cast<char *>(const_cast<void *>(t[i].p)), head * 2, (uint32_t)token * 2};
+    }
+    if (needed > 0 && (!workspace || !aligned(workspace, 16)))
+        return MAXSIM_ERR_INVALID;
+    if (workspace_bytes < needed)
+        return MAXSIM_ERR_SCRATCH;
+    p.q_off = q_offsets;
+    p.k_off = k_offsets;
+    p.b = b;
+    p.q_tokens = q_tokens;
+    p.k_tokens = k_tokens;
+    p.hq = hq;
+    p.hkv = hkv;
+    p.d = d;
+    p.causal = causal != 0;
+    p.scale = scale;
+    p.scale_log2 = scale * 1.44269504088896341f;
+    return MAXSIM_OK;
 }
 
 int forward_common(const void *Q, int n_q, int l_q, const void *D, const int32_t *offsets, int64_t b, int l_d,
@@ -217,7 +285,7 @@ const char *maxsim_strerror(int code)
     case MAXSIM_ERR_INVALID: return "invalid argument (null or misaligned pointer, non-positive size, bad dtype)";
     case MAXSIM_ERR_UNSUPPORTED: return "unsupported shape (an embedding width or a size outside what this entry point is built for)";
     case MAXSIM_ERR_LAUNCH: return "HIP reported an error at kernel launch";
-    case MAXSIM_ERR_SCRATCH: return "sizes exceed the library's static scratch buffer (use the entry point that takes caller buffers)";
+    case MAXSIM_ERR_SCRATCH: return "sizes exceed the library's static scratch buffer (use the entry point that takes caller buffers) or the workspace given";
     default: return "unknown maxsim error code";
     }
 }
@@ -485,6 +553,91 @@ int maxsim_ce_grad(const float *scores, int n, int b, float tau, float *g, float
     if (int rc = ensure_init())
         return rc;
     return finish(maxsim::ce_grad_launch(scores, n, b, tau, g, loss, static_cast<hipStream_t>(stream)));
+}
+
+int maxsim_rope(const void *X, int64_t tokens, int heads, int d, int64_t x_token_stride, int64_t x_head_stride, maxsim_dtype dtype, const float *freqs, int rot,
+                const int32_t *positions, const int32_t *offsets, int64_t b, float scale, int neighbours, int inverse, void *Y, int64_t y_token_stride, int64_t y_head_stride,
+                void *stream)
+{
+    if (!X || !Y || !freqs || tokens < 1 || heads < 1 || d < 2 || rot < 2 || rot > d || rot % 2 != 0 || !dtype_ok((int)dtype) || (offsets && b < 1) || scale != scale)
+        return MAXSIM_ERR_INVALID;
+    if (x_token_stride < 0 || x_head_stride < 0 || y_token_stride < d || y_head_stride < d) // rows of an output lie apart
+        return MAXSIM_ERR_INVALID;
+    const uintptr_t size = dtype == MAXSIM_F32 ? 4 : 2;
+    if (!aligned(X, size) || !aligned(Y, size) || !aligned(freqs, 4) || !aligned(positions, 4) || !aligned(offsets, 4))
+        return MAXSIM_ERR_INVALID;
+    if (!maxsim::rope_width_ok(rot) || tokens >= (int64_t(1) << 31) || b >= (int64_t(1) << 31) || (int64_t)heads * d >= (int64_t(1) << 24))
+        return MAXSIM_ERR_UNSUPPORTED;
+    if (int rc = ensure_init())
+        return rc;
+    return finish(maxsim::rope_launch(X, tokens, heads, d, x_token_stride, x_head_stride, (int)dtype, freqs, rot, positions, offsets, b, scale, neighbours != 0, inverse != 0, Y,
+                                      y_token_stride, y_head_stride, static_cast<hipStream_t>(stream)));
+}
+
+int64_t maxsim_attention_workspace(int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, int hkv, int d)
+{
+    return attention_sizes_ok(b, q_tokens, k_tokens, hq, hkv, d) != MAXSIM_OK ? 0 : maxsim::attention_workspace(b, q_tokens, k_tokens, hq, hkv, d, num_cu());
+}
+
+int maxsim_attention(const void *Q, const void *K, const void *V, const int64_t *strides, const int32_t *q_offsets, const int32_t *k_offsets, int64_t b, int64_t q_tokens,
+                     int64_t k_tokens, int hq, int hkv, int d, maxsim_dtype dtype, int causal, float scale, void *O, float *lse, void *workspace, int64_t workspace_bytes,
+                     void *stream)
+{
+    maxsim::AttnParams p = {};
+    const AttnTensor t[4] = {{&p.Q, Q, hq}, {&p.K, K, hkv}, {&p.V, V, hkv}, {&p.O, O, hq, true}};
+    if (int rc = attention_common(p, t, 4, strides, q_offsets, k_offsets, b, q_tokens, k_tokens, hq, hkv, d, dtype, causal, scale, workspace, workspace_bytes,
+                                  maxsim_attention_workspace(b, q_tokens, k_tokens, hq, hkv, d)))
+        return rc;
+    if (!aligned(lse, 4))
+        return MAXSIM_ERR_INVALID;
+    p.lse = lse;
+    if (int rc = ensure_init())
+        return rc;
+    return finish(maxsim::attention_launch(p, (int)dtype, workspace, num_cu(), static_cast<hipStream_t>(stream)));
+}
+
+int64_t maxsim_attention_backward_workspace(int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, int hkv, int d)
+{
+    return attention_sizes_ok(b, q_tokens, k_tokens, hq, hkv, d) != MAXSIM_OK ? 0 : maxsim::attention_backward_workspace(b, q_tokens, k_tokens, hq, hkv, d, num_cu());
+}
+
+int maxsim_attention_backward(const void *Q, const void *K, const void *V, const void *O, const float *lse, const void *dO, const int64_t *strides, const int32_t *q_offsets,
+                              const int32_t *k_offsets, int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, int hkv, int d, maxsim_dtype dtype, int causal, float scale,
+                              void *dQ, void *dK, void *dV, void *workspace, int64_t workspace_bytes, void *stream)
+{
+    maxsim::AttnParams p = {};
+    const AttnTensor t[8] = {{&p.Q, Q, hq}, {&p.K, K, hkv}, {&p.V, V, hkv}, {&p.O, O, hq}, {&p.dO, dO, hq}, {&p.dQ, dQ, hq, true}, {&p.dK, dK, hkv, true}, {&p.dV, dV, hkv, true}};
+    if (int rc = attention_common(p, t, 8, strides, q_offsets, k_offsets, b, q_tokens, k_tokens, hq, hkv, d, dtype, causal, scale, workspace, workspace_bytes,
+                                  maxsim_attention_backward_workspace(b, q_tokens, k_tokens, hq, hkv, d)))
+        return rc;
+    if (!lse || !aligned(lse, 4))
+        return MAXSIM_ERR_INVALID;
+    p.lse = const_cast<float *>(lse); // (read)
+    if (int rc = ensure_init())
+        return rc;
+    return finish(maxsim::attention_backward_launch(p, (int)dtype, workspace, num_cu(), static_cast<hipStream_t>(stream)));
+}
+
+int64_t maxsim_clip_workspace(int n) { return n < 1 ? 0 : maxsim::clip_workspace(n); }
+
+int maxsim_clip_grad_norm(const void *const *grads, void *const *out, const int64_t *numel, const int32_t *dtypes, int n, float max_norm, float *norm, void *workspace,
+                          int64_t workspace_bytes, void *stream)
+{
+    if (!grads || !out || !numel || !dtypes || n < 1 || !norm || !aligned(norm, 4) || !workspace || !aligned(workspace, 16) || !(max_norm >= 0.0f))
+        return MAXSIM_ERR_INVALID;
+    if (workspace_bytes < maxsim::clip_workspace(n))
+        return MAXSIM_ERR_SCRATCH;
+    int64_t total = 0;
+    for (int i = 0; i < n; ++i) {
+        const uintptr_t size = dtypes[i] == MAXSIM_F32 ? 4 : 2;
+        if (!dtype_ok(dtypes[i]) || numel[i] < 0 || (numel[i] > 0 && (!grads[i] || !out[i])) || !aligned(grads[i], size) || !aligned(out[i], size))
+            return MAXSIM_ERR_INVALID;
+        if (numel[i] > (int64_t(1) << 50) || (total += numel[i]) > (int64_t(1) << 50))
+            return MAXSIM_ERR_UNSUPPORTED;
+    }
+    if (int rc = ensure_init())
+        return rc;
+    return finish(maxsim::clip_launch(grads, out, numel, dtypes, n, max_norm, norm, workspace, static_cast<hipStream_t>(stream)));
 }
 
 } // extern "C"

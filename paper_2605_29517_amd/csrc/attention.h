@@ -1,0 +1,239 @@
+// Shared parts of the attention kernels: packed sequences, tiles in LDS, products.
+//
+// All products are 32x32x16 MFMAs with the tokens of the wavefront's own side as columns, so that a lane keeps ONE of its 32 columns:
+//   scores      S^T [key][query] = K Q^T   (A: rows of K from LDS, B: the query rows, in registers)
+//   values      O^T [d][query]  += V^T P^T (A: V read transposed from LDS, B: P^T, as it left the softmax)
+// A lane (c = lane % 32, h = lane / 32) holds of S^T the rows 8 (r / 4) + 4 h + r % 4, r = 0 .. 15, of column c. Statistics over a
+// column are then in-lane apart from one exchange between the halves, and registers 8 s .. 8 s + 7, rounded to 16 bits, are the
+// B operand of step s of the next product as they are, if its A operand takes the rows in the same order: the transposing read
+// gives a lane four consecutive rows, and rows 4 h .. 4 h + 3 and 8 + 4 h .. 8 + 4 h + 3 are two such reads.
+#pragma once
+#include <algorithm>
+
+#include "common.h"
+
+namespace maxsim {
+
+struct AttnRows { // a packed tensor [tokens, heads, d], strides in bytes
+    char *p;
+    int64_t head;
+    uint32_t token; // (below 2^25: a tile's rows are addressed in 32 bits)
+};
+
+struct AttnParams {
+    AttnRows Q, K, V, O, dO, dQ, dK, dV;
+    const int32_t *q_off, *k_off; // [b + 1]
+    float *lse;                   // [q_tokens, hq]
+    float *part_o, *part_lse;     // [n_split, q_tokens, hq, d], [n_split, q_tokens, hq]: partial results of the split forward
+    float *stat_l, *stat_d;       // [hq, q_tokens]: lse in units of log 2, and delta (the backward's own)
+    int64_t b, q_tokens, k_tokens;
+    int hq, hkv, d;
+    int pack;     // query heads that share a row block: row r of a sequence is token r / pack, head r % pack of the group
+    int n_slots;  // see attn_find_slot
+    int n_split;  // pieces of the keys
+    int causal;
+    float scale, scale_log2; // scale_log2 = scale * log2(e)
+};
+
+// Whether a sequence has tile t of `rows` rows is not known to the host, which has no lengths. Sequence i gets the tile slots
+// [first(i), first(i + 1)), first(i) = floor(offset_i / rows) + i: always as many as it needs and at most one too many, so that the
+// launch is tokens / rows + b tiles and a slot finds its sequence by a search over the offsets. `mul`: rows per token.
+__device__ __forceinline__ int64_t attn_first_slot(const int32_t *off, int64_t i, int64_t tokens, int mul, int rows)
+{
+    return clamp_offset(off[i], 0, tokens) * mul / rows + i;
+}
+// The sequence of a slot: the last i with first(i) <= slot (all lanes active, slot uniform)
+__device__ __forceinline__ int64_t attn_find_slot(const int32_t *off, int64_t b, int64_t tokens, int mul, int rows, int64_t slot)
+{
+    OffsetSearch s; // the first i in [0, b) with first(i) > slot, b if there is none
+    s.begin(b - 1);
+    while (s.open()) {
+        const uint32_t at = s.probe(threadIdx.x & 63);
+        const bool in = at < s.end;
+        const int64_t first = attn_first_slot(off, in ? at : 0u, tokens, mul, rows);
+        s.narrow(__builtin_amdgcn_ballot_w64(in && first <= slot));
+    }
+    const uint32_t i = __builtin_amdgcn_readfirstlane(s.lo);
+    return i ? (int64_t)i - 1 : 0;
+}
+
+// Rows of one sequence
+struct AttnSeq {
+    int64_t start;
+    int len;
+};
+__device__ __forceinline__ AttnSeq attn_seq(const int32_t *off, int64_t i, int64_t tokens)
+{
+    const int64_t s = clamp_offset(off[i], 0, tokens), e = clamp_offset(off[i + 1], s, tokens);
+    return {s, (int)(e - s)};
+}
+
+// A tile of rows in LDS: CH chunks of 16 bytes a row, chunk c of row r at position c ^ swizzle(r). A read of one chunk of eight
+// consecutive rows (the operand as it lies) and a transposing read of 32 bytes of four rows both meet every bank once.
+template <int DP> struct AttnTile {
+    static constexpr int CH = DP / 8, ROW = DP * 2;
+    static __device__ __forceinline__ constexpr int swizzle(int r)
+    {
+        return CH % 8 == 0 ? ((r & 3) << 1) | ((r >> 2) & 1) : (((r >> 1) & 1) << 1) | ((r >> 2) & 1);
+    }
+};
+
+// 16 bytes per lane from base + offset to LDS, lane l's to dst + 16 l (or 4 bytes from any place to dst + 4 l). Assembly, because the compiler puts a wait for all
+// loads into LDS before every LDS read that it cannot tell from their destination, which is the other buffer here; attn_arrive waits
+// for them. No vector register is written; m0, which names the destination, has no other user in these kernels.
+__device__ __forceinline__ uint32_t attn_lds(const void *p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p; }
+__device__ __forceinline__ void attn_load_lds16(const char *base, uint32_t offset, uint32_t dst)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(dst) : "memory");
+}
+__device__ __forceinline__ void attn_load_lds4(const void *src, uint32_t dst)
+{
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(src), "s"(dst) : "memory");
+}
+
+// Copies ROWS consecutive rows of one head to LDS, NW wavefronts together; a wavefront's instruction fills 1 KB. Rows past `last`
+// are the last one's copies and chunks past the row's end are the last chunk's: what is masked later is finite, and of this sequence.
+template <int DP, int ROWS, int NW> struct AttnCopy {
+    static constexpr int CH = DP / 8, N = ROWS * CH / 64, PER = (N + NW - 1) / NW;
+    int row[PER]; // this lane's row, and the byte of its chunk in it, per instruction
+    uint32_t at[PER], full[PER];
+    __device__ __forceinline__ void init(int w, int lane, int d, uint32_t token_stride)
+    {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int p = (w + NW * i) * 64 + lane;
+            row[i] = p / CH;
+            const int c = (p % CH) ^ AttnTile<DP>::swizzle(row[i]);
+            at[i] = min(c, d / 8 - 1) * 16;
+            full[i] = row[i] * token_stride + at[i];
+        }
+    }
+    // rows row0 .. of the head that starts at `head` (uniform); row0 <= last
+    __device__ __forceinline__ void issue(const char *head, uint32_t token_stride, int row0, int last, uint32_t tile, int w) const
+    {
+        const char *base = head + (int64_t)row0 * token_stride;
+        const bool whole = row0 + ROWS - 1 <= last;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            if (N % NW != 0 && w + NW * i >= N)
+                break;
+            attn_load_lds16(base, whole ? full[i] : min(row[i], last - row0) * token_stride + at[i], tile + (w + NW * i) * 1024);
+        }
+    }
+};
+
+// Waits until this wavefront's copies are in LDS and everybody has come here
+__device__ __forceinline__ void attn_arrive()
+{
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+template <int DT> __device__ __forceinline__ void attn_mma(const uint4 &a, const uint4 &b, f32x16 &c) { Traits<fmt(DT, 8)>::mma(a, b, c); }
+
+template <int DT> __device__ __forceinline__ uint32_t attn_pack2(float a, float b)
+{
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    const f32x2 x = {a, b};
+    if constexpr (DT == MAXSIM_F16) {
+        typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, f16x2));
+    } else {
+        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+    }
+}
+template <int DT> __device__ __forceinline__ float attn_float(uint32_t bits16)
+{
+    if constexpr (DT == MAXSIM_F16)
+        return (float)__builtin_bit_cast(_Float16, (uint16_t)bits16);
+    else
+        return __uint_as_float(bits16 << 16);
+}
+// Registers 8 s .. 8 s + 7 of a result as the B operand of step s (rounded to nearest even, 16 bits)
+template <int DT> __device__ __forceinline__ uint4 attn_operand(const f32x16 &x, int s)
+{
+    return make_uint4(attn_pack2<DT>(x[8 * s], x[8 * s + 1]), attn_pack2<DT>(x[8 * s + 2], x[8 * s + 3]), attn_pack2<DT>(x[8 * s + 4], x[8 * s + 5]),
+                      attn_pack2<DT>(x[8 * s + 6], x[8 * s + 7]));
+}
+
+// Where a lane reads a tile's rows as they lie (A operand, chunk 2 u + h of row `32 block + c`)
+template <int DP> struct AttnRowRead {
+    int base, swz;
+    __device__ __forceinline__ AttnRowRead(int lane) : base((lane & 31) * AttnTile<DP>::ROW), swz(AttnTile<DP>::swizzle(lane & 31) ^ (lane >> 5)) {}
+    __device__ __forceinline__ uint4 get(const char *tile, int block, int u) const
+    {
+        return *reinterpret_cast<const uint4 *>(tile + block * 32 * AttnTile<DP>::ROW + base + (((2 * u) ^ swz) << 4));
+    }
+};
+
+// Where a lane reads a tile transposed (A operand: row m = entry 32 block + m of d, k = tile rows 16 s + 4 h + {0 .. 3, 8 .. 11})
+template <int DP> struct AttnColRead {
+    int base, chunk;
+    __device__ __forceinline__ AttnColRead(int lane)
+    {
+        const int i = lane & 15, h = lane >> 5, r = 4 * h + (i >> 2);
+        base = r * AttnTile<DP>::ROW + 8 * (i & 1);
+        chunk = (2 * ((lane >> 4) & 1) + ((i >> 1) & 1)) ^ AttnTile<DP>::swizzle(r);
+    }
+    __device__ __forceinline__ uint4 get(const char *tile, int block, int s) const
+    {
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) s16x4 *lds_ptr;
+        const char *at = tile + s * 16 * AttnTile<DP>::ROW + base + (((4 * block) ^ chunk) << 4);
+        const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)at));
+        const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + 8 * AttnTile<DP>::ROW)));
+        return make_uint4(x.x, x.y, y.x, y.y);
+    }
+};
+
+// Over the two halves of a wavefront: the same in both
+__device__ __forceinline__ float attn_halves_max(float x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float attn_halves_sum(float x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// A lane's part of a row of 16-bit values as the B operand (chunk 2 u + h in step u), zeros past the row's end
+template <int U> __device__ __forceinline__ void attn_load_row(const char *row, int d, int h, uint4 (&x)[U])
+{
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        x[u] = *reinterpret_cast<const uint4 *>(row + min(2 * u + h, d / 8 - 1) * 16);
+}
+// ... and its arrival: before the loop, or the compiler waits in it
+template <int U> __device__ __forceinline__ void attn_have_row(int d, int h, uint4 (&x)[U])
+{
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const bool in = (2 * u + h) * 8 < d;
+        x[u] = make_uint4(in ? x[u].x : 0, in ? x[u].y : 0, in ? x[u].z : 0, in ? x[u].w : 0);
+        asm volatile("" : "+v"(x[u].x), "+v"(x[u].y), "+v"(x[u].z), "+v"(x[u].w));
+    }
+}
+
+// Four consecutive entries of a row
+template <int DT> __device__ __forceinline__ void attn_store4(char *row, int entry, float a, float b, float c, float d)
+{
+    *reinterpret_cast<uint2 *>(row + entry * 2) = make_uint2(attn_pack2<DT>(a, b), attn_pack2<DT>(c, d));
+}
+
+// f(integral_constant DP) for the smallest compiled width that holds d
+template <class F> hipError_t attn_width(int d, F &&f)
+{
+    if (d <= 32)
+        return f(std::integral_constant<int, 32>{});
+    if (d <= 64)
+        return f(std::integral_constant<int, 64>{});
+    if (d <= 96)
+        return f(std::integral_constant<int, 96>{});
+    return f(std::integral_constant<int, 128>{});
+}
+
+} // namespace maxsim

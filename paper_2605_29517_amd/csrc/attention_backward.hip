@@ -1,0 +1,308 @@
+// Gradient of the attention over packed sequences.
+//
+// The probabilities are computed again from the scores and the kept logarithm of their sum: P = exp(scale S - lse). Two kernels, each
+// of which owns what it writes, so that nothing is added in an order that changes from run to run:
+//   dQ      a workgroup owns query rows and walks the keys, as the forward does: S, dP = dO V^T, dS = P (dP - delta), dQ += dS K.
+//           It also leaves delta = sum_d dO O, and lse in units of log 2, for the second kernel.
+//   dK, dV  a workgroup owns keys and walks the queries of all heads that share them: S, dP, dV += P^T dO, dK += dS^T Q.
+// Scores and dP are thus computed twice, seven products instead of five; adding dQ up from the second kernel would need an
+// fp32 array of dQ and atomics. P and dS are rounded to the inputs' type for the last products (as P is in the forward).
+#include "attention.h"
+
+namespace maxsim {
+namespace {
+
+constexpr int NW = 4;
+constexpr int TILE = 64;   // keys per step of the dQ kernel
+constexpr int Q_TILE = 32; // query rows per step of the dK, dV kernel
+constexpr float LOG2E = 1.44269504088896341f;
+
+template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 2) attn_dq_kernel(AttnParams p)
+{
+    constexpr int ROWS = NW * 32, U = DP / 16, NB = DP / 32;
+    constexpr int TILE_BYTES = TILE * DP * 2;
+    __shared__ __attribute__((aligned(16))) char lds[4 * TILE_BYTES]; // two of K, two of V
+
+    const int lane = threadIdx.x & 63, h = lane >> 5;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int v = xcd_grouped(blockIdx.x, gridDim.x); // (as in the forward)
+    const int slot = p.n_slots - 1 - v % p.n_slots, hk = v / p.n_slots;
+
+    const int64_t i = attn_find_slot(p.q_off, p.b, p.q_tokens, p.pack, ROWS, slot);
+    const AttnSeq q = attn_seq(p.q_off, i, p.q_tokens), k = attn_seq(p.k_off, i, p.k_tokens);
+    const int64_t first = (int64_t)(slot - attn_first_slot(p.q_off, i, p.q_tokens, p.pack, ROWS)) * ROWS, rows = (int64_t)q.len * p.pack;
+    if (first < 0 || first >= rows)
+        return;
+
+    const int64_t row = first + w * 32 + (lane & 31);
+    const int64_t row_ok = min(row, rows - 1);
+    const int token = (int)(row_ok / p.pack);
+    const int head = hk * p.pack + (int)(row_ok % p.pack);
+    const int ahead = k.len - q.len;
+    const int limit = p.causal ? max(0, min(k.len, token + ahead + 1)) : k.len;
+    const int64_t wg_last = min(first + ROWS, rows) - 1;
+    const int wg_keys = p.causal ? max(0, min(k.len, (int)(wg_last / p.pack) + ahead + 1)) : k.len;
+    const int wave_keys = __builtin_amdgcn_readlane(limit, 31), all_keys = __builtin_amdgcn_readfirstlane(limit);
+
+    const char *k_head = p.K.p + k.start * p.K.token + hk * p.K.head, *v_head = p.V.p + k.start * p.V.token + hk * p.V.head;
+    AttnCopy<DP, TILE, NW> copy, v_copy;
+    copy.init(w, lane, p.d, p.K.token);
+    v_copy.init(w, lane, p.d, p.V.token);
+    const AttnRowRead<DP> row_read(lane);
+    const AttnColRead<DP> col_read(lane);
+    const int tiles = (wg_keys + TILE - 1) / TILE;
+    auto issue = [&](int t) {
+        const uint32_t to = attn_lds(lds) + (t & 1) * 2 * TILE_BYTES;
+        copy.issue(k_head, p.K.token, t * TILE, k.len - 1, to, w);
+        v_copy.issue(v_head, p.V.token, t * TILE, k.len - 1, to + TILE_BYTES, w);
+    };
+    if (tiles)
+        issue(0);
+
+    uint4 qf[U], gf[U];
+    const int64_t at = q.start + token;
+    attn_load_row(p.Q.p + at * p.Q.token + head * p.Q.head, p.d, h, qf);
+    attn_load_row(p.dO.p + at * p.dO.token + head * p.dO.head, p.d, h, gf);
+    float delta = 0.0f;
+    {
+        uint4 of[U];
+        attn_load_row(p.O.p + at * p.O.token + head * p.O.head, p.d, h, of);
+        attn_have_row(p.d, h, qf);
+        attn_have_row(p.d, h, gf);
+        attn_have_row(p.d, h, of);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t a[4] = {gf[u].x, gf[u].y, gf[u].z, gf[u].w}, b[4] = {of[u].x, of[u].y, of[u].z, of[u].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                delta = __builtin_fmaf(attn_float<DT>(a[e] & 0xffff), attn_float<DT>(b[e] & 0xffff), delta);
+                delta = __builtin_fmaf(attn_float<DT>(a[e] >> 16), attn_float<DT>(b[e] >> 16), delta);
+            }
+        }
+        delta = attn_halves_sum(delta);
+    }
+    float lse2 = p.lse[at * p.hq + head] * LOG2E;
+    asm volatile("" : "+v"(lse2)); // (arrived)
+    if (row < rows && h == 0) {
+        p.stat_l[(int64_t)head * p.q_tokens + at] = lse2;
+        p.stat_d[(int64_t)head * p.q_tokens + at] = delta;
+    }
+
+    f32x16 dq[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            dq[b][r] = 0.0f;
+
+    for (int t = 0; t < tiles; ++t) {
+        attn_arrive();
+        if (t + 1 < tiles)
+            issue(t + 1);
+        const char *kt = lds + (t & 1) * 2 * TILE_BYTES, *vt = kt + TILE_BYTES;
+        const int key0 = t * TILE;
+        if (key0 >= wave_keys)
+            continue;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            f32x16 s, g;
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                s[r] = g[r] = 0.0f;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                attn_mma<DT>(row_read.get(kt, b, u), qf[u], s);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                attn_mma<DT>(row_read.get(vt, b, u), gf[u], g);
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], p.scale_log2, -lse2));
+            if (key0 + 32 * b + 32 > all_keys) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    s[r] = key0 + 32 * b + acc_row(r, h) < limit ? s[r] : 0.0f;
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                s[r] *= g[r] - delta;
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const uint4 ds = attn_operand<DT>(s, x);
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+                    attn_mma<DT>(col_read.get(kt, nb, 2 * b + x), ds, dq[nb]);
+            }
+        }
+    }
+    if (row >= rows)
+        return;
+    char *to = p.dQ.p + at * p.dQ.token + head * p.dQ.head;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4)
+            if (32 * b + 2 * r + 4 * h < p.d)
+                attn_store4<DT>(to, 32 * b + 2 * r + 4 * h, dq[b][r] * p.scale, dq[b][r + 1] * p.scale, dq[b][r + 2] * p.scale, dq[b][r + 3] * p.scale);
+}
+
+// A wavefront owns 32 keys (columns) of one key head.
+template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 1) attn_dkv_kernel(AttnParams p)
+{
+    constexpr int KEYS = NW * 32, U = DP / 16, NB = DP / 32;
+    constexpr int TILE_BYTES = Q_TILE * DP * 2, BUF = 2 * TILE_BYTES + 256; // Q, dO, 32 of lse, 32 of delta
+    __shared__ __attribute__((aligned(16))) char lds[2 * BUF];
+
+    const int lane = threadIdx.x & 63, h = lane >> 5;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int v = xcd_grouped(blockIdx.x, gridDim.x); // (the first tiles, which the most queries see under a causal mask, come first)
+    const int slot = v % p.n_slots, hk = v / p.n_slots;
+
+    const int64_t i = attn_find_slot(p.k_off, p.b, p.k_tokens, 1, KEYS, slot);
+    const AttnSeq q = attn_seq(p.q_off, i, p.q_tokens), k = attn_seq(p.k_off, i, p.k_tokens);
+    const int64_t first_ = (int64_t)(slot - attn_first_slot(p.k_off, i, p.k_tokens, 1, KEYS)) * KEYS;
+    if (first_ < 0 || first_ >= k.len)
+        return;
+    const int first = (int)first_, ahead = k.len - q.len;
+    const int wave_key = first + w * 32, key = wave_key + (lane & 31);
+    const int64_t at = k.start + min(key, k.len - 1);
+
+    // steps: tiles of query rows that see any of the keys, for every head of the group
+    const int q0 = p.causal ? max(0, first - ahead) / Q_TILE : 0, q1 = (q.len + Q_TILE - 1) / Q_TILE;
+    const int per_head = max(0, q1 - q0), steps = per_head * p.pack;
+
+    AttnCopy<DP, Q_TILE, NW> copy, g_copy;
+    copy.init(w, lane, p.d, p.Q.token);
+    g_copy.init(w, lane, p.d, p.dO.token);
+    const AttnRowRead<DP> row_read(lane);
+    const AttnColRead<DP> col_read(lane);
+    int next_g = 0, next_t = q0; // of the next copy
+    auto issue = [&](int n) {
+        const int head = hk * p.pack + next_g, row0 = next_t * Q_TILE;
+        const uint32_t to = attn_lds(lds) + (n & 1) * BUF;
+        copy.issue(p.Q.p + q.start * p.Q.token + head * p.Q.head, p.Q.token, row0, q.len - 1, to, w);
+        g_copy.issue(p.dO.p + q.start * p.dO.token + head * p.dO.head, p.dO.token, row0, q.len - 1, to + TILE_BYTES, w);
+        if (w == 0) {
+            const float *stat = (h ? p.stat_d : p.stat_l) + (int64_t)head * p.q_tokens + q.start + min(row0 + (lane & 31), q.len - 1);
+            attn_load_lds4(stat, to + 2 * TILE_BYTES);
+        }
+        if (++next_t == q1) {
+            next_t = q0;
+            ++next_g;
+        }
+    };
+    if (steps)
+        issue(0);
+
+    uint4 kf[U], vf[U];
+    attn_load_row(p.K.p + at * p.K.token + hk * p.K.head, p.d, h, kf);
+    attn_load_row(p.V.p + at * p.V.token + hk * p.V.head, p.d, h, vf);
+    attn_have_row(p.d, h, kf);
+    attn_have_row(p.d, h, vf);
+    f32x16 dk[NB], dv[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            dk[b][r] = dv[b][r] = 0.0f;
+
+    int tile = q0;
+    for (int n = 0; n < steps; ++n) {
+        attn_arrive();
+        if (n + 1 < steps)
+            issue(n + 1);
+        const char *qt = lds + (n & 1) * BUF, *gt = qt + TILE_BYTES;
+        const float *stat = reinterpret_cast<const float *>(gt + TILE_BYTES);
+        const int row0 = tile * Q_TILE;
+        if (++tile == q1)
+            tile = q0;
+        if (p.causal && row0 + Q_TILE - 1 + ahead < wave_key)
+            continue;
+        f32x16 s, g;
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            s[r] = g[r] = 0.0f;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            attn_mma<DT>(row_read.get(qt, 0, u), kf[u], s);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            attn_mma<DT>(row_read.get(gt, 0, u), vf[u], g);
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const float4 l = *reinterpret_cast<const float4 *>(stat + 2 * r + 4 * h);
+            s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], p.scale_log2, -l.x));
+            s[r + 1] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r + 1], p.scale_log2, -l.y));
+            s[r + 2] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r + 2], p.scale_log2, -l.z));
+            s[r + 3] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r + 3], p.scale_log2, -l.w));
+        }
+        if (row0 + Q_TILE > q.len || (p.causal && row0 + ahead < wave_key + 31)) {
+            const int from = p.causal ? key - ahead : 0; // the first query that sees this lane's key
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int t = row0 + acc_row(r, h);
+                s[r] = t >= from && t < q.len ? s[r] : 0.0f;
+            }
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const uint4 pf = attn_operand<DT>(s, x);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+                attn_mma<DT>(col_read.get(gt, nb, x), pf, dv[nb]);
+        }
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const float4 d = *reinterpret_cast<const float4 *>(stat + 32 + 2 * r + 4 * h);
+            s[r] *= g[r] - d.x;
+            s[r + 1] *= g[r + 1] - d.y;
+            s[r + 2] *= g[r + 2] - d.z;
+            s[r + 3] *= g[r + 3] - d.w;
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const uint4 ds = attn_operand<DT>(s, x);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+                attn_mma<DT>(col_read.get(qt, nb, x), ds, dk[nb]);
+        }
+    }
+    if (key >= k.len)
+        return;
+    char *to_k = p.dK.p + at * p.dK.token + hk * p.dK.head, *to_v = p.dV.p + at * p.dV.token + hk * p.dV.head;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4)
+            if (32 * b + 2 * r + 4 * h < p.d) {
+                attn_store4<DT>(to_k, 32 * b + 2 * r + 4 * h, dk[b][r] * p.scale, dk[b][r + 1] * p.scale, dk[b][r + 2] * p.scale, dk[b][r + 3] * p.scale);
+                attn_store4<DT>(to_v, 32 * b + 2 * r + 4 * h, dv[b][r], dv[b][r + 1], dv[b][r + 2], dv[b][r + 3]);
+            }
+}
+
+} // namespace
+
+int64_t attention_backward_workspace(int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, int hkv, int d, int num_cu) { return 2 * q_tokens * hq * 4; }
+
+hipError_t attention_backward_launch(AttnParams p, int dtype, void *workspace, int num_cu, hipStream_t stream)
+{
+    p.pack = p.hq / p.hkv;
+    p.stat_l = static_cast<float *>(workspace);
+    p.stat_d = p.stat_l + p.q_tokens * p.hq;
+    return attn_width(p.d, [&](auto dp) {
+        constexpr int DP = decltype(dp)::value;
+        p.n_slots = (int)(p.q_tokens * p.pack / (NW * 32) + p.b);
+        if (dtype == MAXSIM_F16)
+            attn_dq_kernel<MAXSIM_F16, DP><<<(unsigned)(p.n_slots * p.hkv), NW * 64, 0, stream>>>(p);
+        else
+            attn_dq_kernel<MAXSIM_BF16, DP><<<(unsigned)(p.n_slots * p.hkv), NW * 64, 0, stream>>>(p);
+        p.n_slots = (int)(p.k_tokens / (NW * 32) + p.b);
+        if (dtype == MAXSIM_F16)
+            attn_dkv_kernel<MAXSIM_F16, DP><<<(unsigned)(p.n_slots * p.hkv), NW * 64, 0, stream>>>(p);
+        else
+            attn_dkv_kernel<MAXSIM_BF16, DP><<<(unsigned)(p.n_slots * p.hkv), NW * 64, 0, stream>>>(p);
+        return hipGetLastError();
+    });
+}
+
+} // namespace maxsim

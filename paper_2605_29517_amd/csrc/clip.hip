@@ -1,0 +1,238 @@
+// Clipping by the global norm: n = sqrt(sum g^2) over all gradients, g = min(1, max_norm / (n + 1e-6)) g.
+//
+// Two passes over the gradients, which is what the definition needs: one for the sum, one for the product. The tensors are cut into
+// chunks of CHUNK entries, and every workgroup takes a contiguous range of the chunks of all tensors, so that many small
+// tensors and a few large ones fill the chip alike. Squares are added in 64 bits (no overflow at any fp32 value; the adders keep up
+// with the memory four times over), each workgroup's sum goes to a place of its own and the second pass adds these in a
+// fixed order in every workgroup: the same bits every time, without atomics or a launch in between. The second pass walks its range
+// backwards: what the first one read last is what the caches still hold.
+//
+// Compiled with NaNs honoured: a gradient that is not finite has to show in the norm.
+#include <algorithm>
+
+#include "common.h"
+
+namespace maxsim {
+
+constexpr int CLIP_TENSORS = 110; // that fit the arguments of a launch (4 KB)
+
+struct ClipTensors {
+    const void *g[CLIP_TENSORS];
+    void *out[CLIP_TENSORS];
+    int64_t numel[CLIP_TENSORS];
+    int64_t chunk[CLIP_TENSORS]; // first chunk of the tensor among those of all
+    int32_t dtype[CLIP_TENSORS];
+};
+// The same in memory, for any number of tensors
+struct ClipTable {
+    const void **g;
+    void **out;
+    int64_t *numel, *chunk;
+    int32_t *dtype;
+};
+
+namespace {
+
+constexpr int WG = 256;
+constexpr int CHUNK = 4096;
+constexpr int MAX_WG = 2048; // eight to a compute unit, all resident at a time
+
+template <class T> __device__ __forceinline__ double to_double(T x) { return (double)(float)x; }
+
+// f(values of 16 bytes as floats, ...) over the entries [0, n) of a chunk; entries may lie at any address that is a multiple of their size
+template <class T> struct Vec {
+    static constexpr int V = 16 / sizeof(T);
+    T x[V];
+};
+template <class T> __device__ __forceinline__ Vec<T> load_vec(const T *p)
+{
+    Vec<T> r;
+    __builtin_memcpy(&r, p, 16);
+    return r;
+}
+template <class T> __device__ __forceinline__ void store_vec(T *p, const Vec<T> &r) { __builtin_memcpy(p, &r, 16); }
+
+template <class T> __device__ __forceinline__ double chunk_squares(const T *g, int n)
+{
+    constexpr int V = Vec<T>::V, STEPS = CHUNK / (WG * V);
+    double sum = 0.0;
+    if (n == CHUNK) {
+        Vec<T> x[STEPS];
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+            x[s] = load_vec(g + (s * WG + threadIdx.x) * V);
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const double v = to_double(x[s].x[i]);
+                sum = __builtin_fma(v, v, sum);
+            }
+    } else {
+        for (int e = threadIdx.x; e < n; e += WG) {
+            const double v = to_double(g[e]);
+            sum = __builtin_fma(v, v, sum);
+        }
+    }
+    return sum;
+}
+template <class T> __device__ __forceinline__ void chunk_scaled(const T *g, T *out, int n, float by)
+{
+    constexpr int V = Vec<T>::V, STEPS = CHUNK / (WG * V);
+    if (n == CHUNK) {
+        Vec<T> x[STEPS];
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+            x[s] = load_vec(g + (s * WG + threadIdx.x) * V);
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                x[s].x[i] = (T)((float)x[s].x[i] * by);
+            store_vec(out + (s * WG + threadIdx.x) * V, x[s]);
+        }
+    } else {
+        for (int e = threadIdx.x; e < n; e += WG)
+            out[e] = (T)((float)g[e] * by);
+    }
+}
+
+__device__ __forceinline__ double wave_sum(double x)
+{
+#pragma unroll
+    for (int m = 32; m; m >>= 1)
+        x += __shfl_xor(x, m, 64);
+    return x;
+}
+__device__ __forceinline__ double wg_sum(double x) // the same in every thread
+{
+    __shared__ double part[WG / 64];
+    x = wave_sum(x);
+    if ((threadIdx.x & 63) == 0)
+        part[threadIdx.x >> 6] = x;
+    __syncthreads();
+    double s = 0.0;
+    for (int w = 0; w < WG / 64; ++w)
+        s += part[w];
+    return s;
+}
+
+// The tensor that a chunk lies in: the last one whose first chunk is not after it (tensors without entries share their first chunk with
+// the next one and are never the last)
+template <class Tensors> __device__ __forceinline__ int find_tensor(const Tensors &t, int n, int64_t chunk)
+{
+    int lo = 0, hi = n; // the first tensor that starts after the chunk
+    while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        if (t.chunk[mid] > chunk)
+            hi = mid;
+        else
+            lo = mid + 1;
+    }
+    return lo - 1;
+}
+
+template <class Tensors> __global__ void __launch_bounds__(WG) clip_sum_kernel(Tensors t, int n, int64_t chunks, double *part)
+{
+    const int64_t c0 = chunks * blockIdx.x / gridDim.x, c1 = chunks * (blockIdx.x + 1) / gridDim.x;
+    int i = find_tensor(t, n, c0);
+    double sum = 0.0;
+    for (int64_t c = c0; c < c1; ++c) {
+        while (i + 1 < n && t.chunk[i + 1] <= c)
+            ++i;
+        const int64_t e = (c - t.chunk[i]) * CHUNK, left = t.numel[i] - e;
+        const int m = left < CHUNK ? (int)left : CHUNK;
+        if (t.dtype[i] == MAXSIM_F32)
+            sum += chunk_squares(static_cast<const float *>(t.g[i]) + e, m);
+        else if (t.dtype[i] == MAXSIM_F16)
+            sum += chunk_squares(static_cast<const _Float16 *>(t.g[i]) + e, m);
+        else
+            sum += chunk_squares(static_cast<const __bf16 *>(t.g[i]) + e, m);
+    }
+    sum = wg_sum(sum);
+    if (threadIdx.x == 0)
+        part[blockIdx.x] = sum;
+}
+
+template <class Tensors> __global__ void __launch_bounds__(WG) clip_scale_kernel(Tensors t, int n, int64_t chunks, const double *part, int parts, float max_norm, float *norm)
+{
+    double sum = 0.0;
+    for (int x = threadIdx.x; x < parts; x += WG)
+        sum += part[x];
+    const float total = (float)sqrt(wg_sum(sum));
+    if (blockIdx.x == 0 && threadIdx.x == 0)
+        *norm = total;
+    const float by0 = max_norm / (total + 1e-6f);
+    const float by = by0 < 1.0f || by0 != by0 ? by0 : 1.0f;
+    const int64_t c0 = chunks * blockIdx.x / gridDim.x, c1 = chunks * (blockIdx.x + 1) / gridDim.x;
+    if (c0 >= c1)
+        return;
+    int i = find_tensor(t, n, c1 - 1);
+    for (int64_t c = c1 - 1; c >= c0; --c) {
+        while (t.chunk[i] > c)
+            --i;
+        if (by == 1.0f && t.out[i] == t.g[i]) // nothing changes
+            continue;
+        const int64_t e = (c - t.chunk[i]) * CHUNK, left = t.numel[i] - e;
+        const int m = left < CHUNK ? (int)left : CHUNK;
+        if (t.dtype[i] == MAXSIM_F32)
+            chunk_scaled(static_cast<const float *>(t.g[i]) + e, static_cast<float *>(t.out[i]) + e, m, by);
+        else if (t.dtype[i] == MAXSIM_F16)
+            chunk_scaled(static_cast<const _Float16 *>(t.g[i]) + e, static_cast<_Float16 *>(t.out[i]) + e, m, by);
+        else
+            chunk_scaled(static_cast<const __bf16 *>(t.g[i]) + e, static_cast<__bf16 *>(t.out[i]) + e, m, by);
+    }
+}
+
+// A part of the table from the launch's arguments into memory
+__global__ void __launch_bounds__(128) clip_table_kernel(ClipTensors t, int n, ClipTable to, int first)
+{
+    const int i = threadIdx.x;
+    if (i < n) {
+        to.g[first + i] = t.g[i];
+        to.out[first + i] = t.out[i];
+        to.numel[first + i] = t.numel[i];
+        to.chunk[first + i] = t.chunk[i];
+        to.dtype[first + i] = t.dtype[i];
+    }
+}
+
+} // namespace
+
+int64_t clip_workspace(int n) { return MAX_WG * 8 + (n > CLIP_TENSORS ? (int64_t)n * 36 : 0); }
+
+hipError_t clip_launch(const void *const *g, void *const *out, const int64_t *numel, const int32_t *dtype, int n, float max_norm, float *norm, void *workspace, hipStream_t stream)
+{
+    double *part = static_cast<double *>(workspace);
+    char *at = reinterpret_cast<char *>(part + MAX_WG);
+    ClipTable table = {reinterpret_cast<const void **>(at), reinterpret_cast<void **>(at + 8 * (int64_t)n), reinterpret_cast<int64_t *>(at + 16 * (int64_t)n),
+                       reinterpret_cast<int64_t *>(at + 24 * (int64_t)n), reinterpret_cast<int32_t *>(at + 32 * (int64_t)n)};
+    int64_t chunks = 0;
+    ClipTensors t = {};
+    int held = 0;
+    for (int i = 0; i < n; ++i) {
+        if (held == CLIP_TENSORS) {
+            clip_table_kernel<<<1, 128, 0, stream>>>(t, held, table, i - held);
+            held = 0;
+        }
+        t.g[held] = g[i];
+        t.out[held] = out[i];
+        t.numel[held] = numel[i];
+        t.chunk[held] = chunks;
+        t.dtype[held] = dtype[i];
+        ++held;
+        chunks += (numel[i] + CHUNK - 1) / CHUNK;
+    }
+    const unsigned grid = (unsigned)std::max<int64_t>(1, std::min<int64_t>(chunks, MAX_WG));
+    if (n <= CLIP_TENSORS) {
+        clip_sum_kernel<<<grid, WG, 0, stream>>>(t, n, chunks, part);
+        clip_scale_kernel<<<grid, WG, 0, stream>>>(t, n, chunks, part, (int)grid, max_norm, norm);
+    } else {
+        clip_table_kernel<<<1, 128, 0, stream>>>(t, held, table, n - held);
+        clip_sum_kernel<<<grid, WG, 0, stream>>>(table, n, chunks, part);
+        clip_scale_kernel<<<grid, WG, 0, stream>>>(table, n, chunks, part, (int)grid, max_norm, norm);
+    }
+    return hipGetLastError();
+}
+
+} // namespace maxsim
