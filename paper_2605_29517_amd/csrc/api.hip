@@ -612,6 +612,8 @@ int maxsim_attention_backward(const void *Q, const void *K, const void *V, const
         return rc;
     if (!lse || !aligned(lse, 4))
         return MAXSIM_ERR_INVALID;
+    if (q_tokens >= (int64_t(1) << 30)) // two rows of q_tokens floats are addressed in 32 bits
+        return MAXSIM_ERR_UNSUPPORTED;
     p.lse = const_cast<float *>(lse); // (read)
     if (int rc = ensure_init())
         return rc;

@@ -25,7 +25,7 @@ struct AttnParams {
     const int32_t *q_off, *k_off; // [b + 1]
     float *lse;                   // [q_tokens, hq]
     float *part_o, *part_lse;     // [n_split, q_tokens, hq, d], [n_split, q_tokens, hq]: partial results of the split forward
-    float *stat_l, *stat_d;       // [hq, q_tokens]: lse in units of log 2, and delta (the backward's own)
+    float *stat;                  // [hq, 2, q_tokens]: -lse / scale and -delta (the backward's own)
     int64_t b, q_tokens, k_tokens;
     int hq, hkv, d;
     int pack;     // query heads that share a row block: row r of a sequence is token r / pack, head r % pack of the group
@@ -78,7 +78,7 @@ template <int DP> struct AttnTile {
     }
 };
 
-// 16 bytes per lane from base + offset to LDS, lane l's to dst + 16 l (or 4 bytes from any place to dst + 4 l). Assembly, because the compiler puts a wait for all
+// 16 (or 4) bytes per lane from base + offset to LDS, lane l's to dst + 16 l (4 l). Assembly, because the compiler puts a wait for all
 // loads into LDS before every LDS read that it cannot tell from their destination, which is the other buffer here; attn_arrive waits
 // for them. No vector register is written; m0, which names the destination, has no other user in these kernels.
 __device__ __forceinline__ uint32_t attn_lds(const void *p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p; }
@@ -86,38 +86,39 @@ __device__ __forceinline__ void attn_load_lds16(const char *base, uint32_t offse
 {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(dst) : "memory");
 }
-__device__ __forceinline__ void attn_load_lds4(const void *src, uint32_t dst)
+__device__ __forceinline__ void attn_load_lds4(const void *base, uint32_t offset, uint32_t dst)
 {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(src), "s"(dst) : "memory");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(offset), "s"(base), "s"(dst) : "memory");
 }
 
 // Copies ROWS consecutive rows of one head to LDS, NW wavefronts together; a wavefront's instruction fills 1 KB. Rows past `last`
 // are the last one's copies and chunks past the row's end are the last chunk's: what is masked later is finite, and of this sequence.
 template <int DP, int ROWS, int NW> struct AttnCopy {
     static constexpr int CH = DP / 8, N = ROWS * CH / 64, PER = (N + NW - 1) / NW;
-    int row[PER]; // this lane's row, and the byte of its chunk in it, per instruction
-    uint32_t at[PER], full[PER];
-    __device__ __forceinline__ void init(int w, int lane, int d, uint32_t token_stride)
+    static constexpr bool EVEN = NW * 64 % (8 * CH) == 0; // a lane's rows are STEP apart, its chunk is the same in all of them
+    static constexpr int STEP = NW * 64 / CH, HELD = EVEN ? 1 : PER;
+    int row[HELD]; // this lane's row, and the byte of its chunk in it, per instruction
+    uint32_t at[HELD];
+    __device__ __forceinline__ void init(int w, int lane, int d)
     {
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
+        for (int i = 0; i < HELD; ++i) {
             const int p = (w + NW * i) * 64 + lane;
             row[i] = p / CH;
             const int c = (p % CH) ^ AttnTile<DP>::swizzle(row[i]);
             at[i] = min(c, d / 8 - 1) * 16;
-            full[i] = row[i] * token_stride + at[i];
         }
     }
     // rows row0 .. of the head that starts at `head` (uniform); row0 <= last
     __device__ __forceinline__ void issue(const char *head, uint32_t token_stride, int row0, int last, uint32_t tile, int w) const
     {
         const char *base = head + (int64_t)row0 * token_stride;
-        const bool whole = row0 + ROWS - 1 <= last;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             if (N % NW != 0 && w + NW * i >= N)
                 break;
-            attn_load_lds16(base, whole ? full[i] : min(row[i], last - row0) * token_stride + at[i], tile + (w + NW * i) * 1024);
+            const int r = EVEN ? row[0] + STEP * i : row[EVEN ? 0 : i];
+            attn_load_lds16(base, (uint32_t)min(r, last - row0) * token_stride + at[EVEN ? 0 : i], tile + (w + NW * i) * 1024);
         }
     }
 };

@@ -53,9 +53,7 @@ template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, 2) 
 
     const char *k_head = p.K.p + k.start * p.K.token + hk * p.K.head, *v_head = p.V.p + k.start * p.V.token + hk * p.V.head;
     AttnCopy<DP, TILE, NW> copy;
-    copy.init(w, lane, p.d, p.K.token);
-    AttnCopy<DP, TILE, NW> v_copy;
-    v_copy.init(w, lane, p.d, p.V.token);
+    copy.init(w, lane, p.d);
     const AttnRowRead<DP> k_read(lane);
     const AttnColRead<DP> v_read(lane);
 
@@ -72,7 +70,7 @@ template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, 2) 
     auto issue = [&](int t) {
         const uint32_t to = attn_lds(lds) + (t & 1) * 2 * TILE_BYTES;
         copy.issue(k_head, p.K.token, t * TILE, k.len - 1, to, w);
-        v_copy.issue(v_head, p.V.token, t * TILE, k.len - 1, to + TILE_BYTES, w);
+        copy.issue(v_head, p.V.token, t * TILE, k.len - 1, to + TILE_BYTES, w);
     };
     if (t0 < t1)
         issue(t0);

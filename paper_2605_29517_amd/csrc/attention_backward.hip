@@ -3,7 +3,7 @@
 // The probabilities are computed again from the scores and the kept logarithm of their sum: P = exp(scale S - lse). Two kernels, each
 // of which owns what it writes, so that nothing is added in an order that changes from run to run:
 //   dQ      a workgroup owns query rows and walks the keys, as the forward does: S, dP = dO V^T, dS = P (dP - delta), dQ += dS K.
-//           It also leaves delta = sum_d dO O, and lse in units of log 2, for the second kernel.
+//           It also leaves what the second kernel's sums start from, -lse / scale and -delta = -sum_d dO O.
 //   dK, dV  a workgroup owns keys and walks the queries of all heads that share them: S, dP, dV += P^T dO, dK += dS^T Q.
 // Scores and dP are thus computed twice, seven products instead of five; adding dQ up from the second kernel would need an
 // fp32 array of dQ and atomics. P and dS are rounded to the inputs' type for the last products (as P is in the forward).
@@ -45,16 +45,15 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 2) attn_dq_
     const int wave_keys = __builtin_amdgcn_readlane(limit, 31), all_keys = __builtin_amdgcn_readfirstlane(limit);
 
     const char *k_head = p.K.p + k.start * p.K.token + hk * p.K.head, *v_head = p.V.p + k.start * p.V.token + hk * p.V.head;
-    AttnCopy<DP, TILE, NW> copy, v_copy;
-    copy.init(w, lane, p.d, p.K.token);
-    v_copy.init(w, lane, p.d, p.V.token);
+    AttnCopy<DP, TILE, NW> copy;
+    copy.init(w, lane, p.d);
     const AttnRowRead<DP> row_read(lane);
     const AttnColRead<DP> col_read(lane);
     const int tiles = (wg_keys + TILE - 1) / TILE;
     auto issue = [&](int t) {
         const uint32_t to = attn_lds(lds) + (t & 1) * 2 * TILE_BYTES;
         copy.issue(k_head, p.K.token, t * TILE, k.len - 1, to, w);
-        v_copy.issue(v_head, p.V.token, t * TILE, k.len - 1, to + TILE_BYTES, w);
+        copy.issue(v_head, p.V.token, t * TILE, k.len - 1, to + TILE_BYTES, w);
     };
     if (tiles)
         issue(0);
@@ -83,10 +82,8 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 2) attn_dq_
     }
     float lse2 = p.lse[at * p.hq + head] * LOG2E;
     asm volatile("" : "+v"(lse2)); // (arrived)
-    if (row < rows && h == 0) {
-        p.stat_l[(int64_t)head * p.q_tokens + at] = lse2;
-        p.stat_d[(int64_t)head * p.q_tokens + at] = delta;
-    }
+    if (row < rows)
+        p.stat[(2 * (int64_t)head + h) * p.q_tokens + at] = h ? -delta : -lse2 / p.scale_log2;
 
     f32x16 dq[NB];
 #pragma unroll
@@ -107,8 +104,10 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 2) attn_dq_
         for (int b = 0; b < 2; ++b) {
             f32x16 s, g;
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                s[r] = g[r] = 0.0f;
+            for (int r = 0; r < 16; ++r) {
+                s[r] = 0.0f;
+                g[r] = -delta; // (dP - delta: the sums start there)
+            }
 #pragma unroll
             for (int u = 0; u < U; ++u)
                 attn_mma<DT>(row_read.get(kt, b, u), qf[u], s);
@@ -125,7 +124,7 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 2) attn_dq_
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r)
-                s[r] *= g[r] - delta;
+                s[r] *= g[r];
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 const uint4 ds = attn_operand<DT>(s, x);
@@ -147,10 +146,10 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 2) attn_dq_
 }
 
 // A wavefront owns 32 keys (columns) of one key head.
-template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 1) attn_dkv_kernel(AttnParams p)
+template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 2) attn_dkv_kernel(AttnParams p)
 {
     constexpr int KEYS = NW * 32, U = DP / 16, NB = DP / 32;
-    constexpr int TILE_BYTES = Q_TILE * DP * 2, BUF = 2 * TILE_BYTES + 256; // Q, dO, 32 of lse, 32 of delta
+    constexpr int TILE_BYTES = Q_TILE * DP * 2, BUF = 2 * TILE_BYTES + 256; // Q, dO, 32 of -lse / scale, 32 of -delta
     __shared__ __attribute__((aligned(16))) char lds[2 * BUF];
 
     const int lane = threadIdx.x & 63, h = lane >> 5;
@@ -171,9 +170,8 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 1) attn_dkv
     const int q0 = p.causal ? max(0, first - ahead) / Q_TILE : 0, q1 = (q.len + Q_TILE - 1) / Q_TILE;
     const int per_head = max(0, q1 - q0), steps = per_head * p.pack;
 
-    AttnCopy<DP, Q_TILE, NW> copy, g_copy;
-    copy.init(w, lane, p.d, p.Q.token);
-    g_copy.init(w, lane, p.d, p.dO.token);
+    AttnCopy<DP, Q_TILE, NW> copy;
+    copy.init(w, lane, p.d);
     const AttnRowRead<DP> row_read(lane);
     const AttnColRead<DP> col_read(lane);
     int next_g = 0, next_t = q0; // of the next copy
@@ -181,11 +179,9 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 1) attn_dkv
         const int head = hk * p.pack + next_g, row0 = next_t * Q_TILE;
         const uint32_t to = attn_lds(lds) + (n & 1) * BUF;
         copy.issue(p.Q.p + q.start * p.Q.token + head * p.Q.head, p.Q.token, row0, q.len - 1, to, w);
-        g_copy.issue(p.dO.p + q.start * p.dO.token + head * p.dO.head, p.dO.token, row0, q.len - 1, to + TILE_BYTES, w);
-        if (w == 0) {
-            const float *stat = (h ? p.stat_d : p.stat_l) + (int64_t)head * p.q_tokens + q.start + min(row0 + (lane & 31), q.len - 1);
-            attn_load_lds4(stat, to + 2 * TILE_BYTES);
-        }
+        copy.issue(p.dO.p + q.start * p.dO.token + head * p.dO.head, p.dO.token, row0, q.len - 1, to + TILE_BYTES, w);
+        if (w == 0)
+            attn_load_lds4(p.stat + 2 * (int64_t)head * p.q_tokens + q.start + row0, (uint32_t)(min(lane & 31, q.len - 1 - row0) + h * (int)p.q_tokens) * 4, to + 2 * TILE_BYTES);
         if (++next_t == q1) {
             next_t = q0;
             ++next_g;
@@ -212,30 +208,33 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 1) attn_dkv
         if (n + 1 < steps)
             issue(n + 1);
         const char *qt = lds + (n & 1) * BUF, *gt = qt + TILE_BYTES;
-        const float *stat = reinterpret_cast<const float *>(gt + TILE_BYTES);
+        const f32x4 *stat = reinterpret_cast<const f32x4 *>(gt + TILE_BYTES);
         const int row0 = tile * Q_TILE;
         if (++tile == q1)
             tile = q0;
         if (p.causal && row0 + Q_TILE - 1 + ahead < wave_key)
             continue;
+        // the sums start from what is subtracted from them: S - lse / scale, dP - delta
         f32x16 s, g;
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-            s[r] = g[r] = 0.0f;
+        for (int r = 0; r < 16; r += 4) {
+            const f32x4 l = stat[r / 2 + h];
+            s[r] = l[0], s[r + 1] = l[1], s[r + 2] = l[2], s[r + 3] = l[3];
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u)
             attn_mma<DT>(row_read.get(qt, 0, u), kf[u], s);
 #pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const f32x4 d = stat[8 + r / 2 + h];
+            g[r] = d[0], g[r + 1] = d[1], g[r + 2] = d[2], g[r + 3] = d[3];
+        }
+#pragma unroll
         for (int u = 0; u < U; ++u)
             attn_mma<DT>(row_read.get(gt, 0, u), vf[u], g);
 #pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-            const float4 l = *reinterpret_cast<const float4 *>(stat + 2 * r + 4 * h);
-            s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], p.scale_log2, -l.x));
-            s[r + 1] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r + 1], p.scale_log2, -l.y));
-            s[r + 2] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r + 2], p.scale_log2, -l.z));
-            s[r + 3] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r + 3], p.scale_log2, -l.w));
-        }
+        for (int r = 0; r < 16; ++r)
+            s[r] = __builtin_amdgcn_exp2f(s[r] * p.scale_log2);
         if (row0 + Q_TILE > q.len || (p.causal && row0 + ahead < wave_key + 31)) {
             const int from = p.causal ? key - ahead : 0; // the first query that sees this lane's key
 #pragma unroll
@@ -252,13 +251,8 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 1) attn_dkv
                 attn_mma<DT>(col_read.get(gt, nb, x), pf, dv[nb]);
         }
 #pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-            const float4 d = *reinterpret_cast<const float4 *>(stat + 32 + 2 * r + 4 * h);
-            s[r] *= g[r] - d.x;
-            s[r + 1] *= g[r + 1] - d.y;
-            s[r + 2] *= g[r + 2] - d.z;
-            s[r + 3] *= g[r + 3] - d.w;
-        }
+        for (int r = 0; r < 16; ++r)
+            s[r] *= g[r];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
             const uint4 ds = attn_operand<DT>(s, x);
@@ -282,13 +276,12 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 1) attn_dkv
 
 } // namespace
 
-int64_t attention_backward_workspace(int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, int hkv, int d, int num_cu) { return 2 * q_tokens * hq * 4; }
+int64_t attention_backward_workspace(int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, int hkv, int d, int num_cu) { return q_tokens * hq * 8; }
 
 hipError_t attention_backward_launch(AttnParams p, int dtype, void *workspace, int num_cu, hipStream_t stream)
 {
     p.pack = p.hq / p.hkv;
-    p.stat_l = static_cast<float *>(workspace);
-    p.stat_d = p.stat_l + p.q_tokens * p.hq;
+    p.stat = static_cast<float *>(workspace);
     return attn_width(p.d, [&](auto dp) {
         constexpr int DP = decltype(dp)::value;
         p.n_slots = (int)(p.q_tokens * p.pack / (NW * 32) + p.b);
