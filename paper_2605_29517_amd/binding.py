@@ -93,7 +93,9 @@ def load():
     native = _load_native()
     if native is not None:
         native.bind(*(ctypes.cast(f, p).value for f in (L.maxsim_forward, L.maxsim_forward_ragged, L.maxsim_backward, L.maxsim_backward_ragged, L.maxsim_ce_grad,
-                                                        L.maxsim_quantize_rows_i8, L.maxsim_forward_i8, L.maxsim_forward_i8_ragged)))
+                                                        L.maxsim_quantize_rows_i8, L.maxsim_forward_i8, L.maxsim_forward_i8_ragged, L.maxsim_rope,
+                                                        L.maxsim_attention_workspace, L.maxsim_attention, L.maxsim_attention_backward_workspace, L.maxsim_attention_backward,
+                                                        L.maxsim_clip_workspace, L.maxsim_clip_grad_norm)))
     _lib, _native = L, native
     return L
 
@@ -156,13 +158,12 @@ def _stream(t: torch.Tensor):
     return torch._C._cuda_getCurrentRawStream(t.device.index)
 
 
-class _on_device:
-    """Makes the tensor's GPU current for the call; rejects host tensors before anything else."""
+class _gpu:
+    """Makes the tensor's GPU current for the call."""
 
     __slots__ = ("_ctx",)
 
-    def __init__(self, t, name):
-        _dev(t, name)
+    def __init__(self, t):
         self._ctx = None if t.device.index == torch.cuda.current_device() else torch.cuda.device(t.device)
 
     def __enter__(self):
@@ -172,6 +173,16 @@ class _on_device:
     def __exit__(self, *a):
         if self._ctx is not None:
             self._ctx.__exit__(*a)
+
+
+class _on_device(_gpu):
+    """... and rejects host tensors before anything else."""
+
+    __slots__ = ()
+
+    def __init__(self, t, name):
+        _dev(t, name)
+        super().__init__(t)
 
 
 def maxsim_forward(Q, D, scores=None, argmax=None, want_argmax=False):
@@ -539,6 +550,10 @@ def maxsim_rope(X, freqs, positions=None, offsets=None, interleaved=False, inver
     2 * len(freqs) entries of each head turn by position * freqs, in halves (i, i + rot / 2) or neighbours (interleaved).  Positions are
     given (int32 [tokens]), or a token's place in its sequence (offsets int32 [b + 1]), or its row.  inverse: the gradient's
     direction.  out may be X."""
+    if _native is not None:
+        r = _native.rope(X, freqs, positions, offsets, interleaved, inverse, scale, out)
+        if r is not None:
+            return r if type(r) is not int else _check(r, "maxsim_rope")
     L = load()
     xt, xh = _rows(X, "X")
     T, H, d = X.shape
@@ -555,7 +570,7 @@ def maxsim_rope(X, freqs, positions=None, offsets=None, interleaved=False, inver
     if offsets is not None and (offsets.dim() != 1 or offsets.shape[0] < 2):
         raise MaxSimError("offsets must hold b + 1 >= 2 entries")
     _same_device(X, freqs=freqs, positions=positions, offsets=offsets, out=out)
-    with torch.cuda.device(X.device):
+    with _gpu(X):
         rc = L.maxsim_rope(X.data_ptr(), T, H, d, xt, xh, _DTYPE[X.dtype], _dev(freqs, "freqs", torch.float32), 2 * freqs.shape[0],
                            _dev(positions, "positions", torch.int32) if positions is not None else None,
                            _dev(offsets, "offsets", torch.int32) if offsets is not None else None, offsets.shape[0] - 1 if offsets is not None else 0,
@@ -593,6 +608,10 @@ def maxsim_attention(Q, K, V, q_offsets, k_offsets=None, causal=True, scale=None
     """Attention over packed sequences: Q [q_tokens, hq, d], K and V [k_tokens, hkv, d] (fp16 or bf16; views may be given), int32 offsets
     [b + 1] (k_offsets: q_offsets where the same tokens are queries and keys) -> (O like Q, lse fp32 [q_tokens, hq]).  scale: 1 / sqrt(d)
     where it is not given."""
+    if _native is not None:
+        r = _native.attention(Q, K, V, q_offsets, k_offsets, causal, scale, out, lse, workspace)
+        if r is not None:
+            return r if type(r) is not int else _check(r, "maxsim_attention")
     L = load()
     strides, q_offsets, k_offsets, sizes, scale = _attention_sizes(Q, K, V, q_offsets, k_offsets, scale)
     if out is None:
@@ -602,7 +621,7 @@ def maxsim_attention(Q, K, V, q_offsets, k_offsets=None, causal=True, scale=None
     strides += _rows(out, "out", Q.shape, Q.dtype)
     _same(lse, "lse", Q.shape[:2], torch.float32)
     _same_device(Q, K=K, V=V, q_offsets=q_offsets, k_offsets=k_offsets, out=out, lse=lse)
-    with torch.cuda.device(Q.device):
+    with _gpu(Q):
         ws = _workspace(workspace, L.maxsim_attention_workspace(*sizes), Q)
         rc = L.maxsim_attention(Q.data_ptr(), K.data_ptr(), V.data_ptr(), (ctypes.c_int64 * 8)(*strides), _dev(q_offsets, "q_offsets", torch.int32),
                                 _dev(k_offsets, "k_offsets", torch.int32), *sizes, _DTYPE[Q.dtype], int(bool(causal)), scale, out.data_ptr(), _dev(lse, "lse"),
@@ -613,6 +632,10 @@ def maxsim_attention(Q, K, V, q_offsets, k_offsets=None, causal=True, scale=None
 
 def maxsim_attention_backward(Q, K, V, out, lse, dout, q_offsets, k_offsets=None, causal=True, scale=None, dQ=None, dK=None, dV=None, workspace=None):
     """The gradient of maxsim_attention (out and lse as it left them) -> (dQ, dK, dV) in the inputs' type."""
+    if _native is not None:
+        r = _native.attention_backward(Q, K, V, out, lse, dout, q_offsets, k_offsets, causal, scale, dQ, dK, dV, workspace)
+        if r is not None:
+            return r if type(r) is not int else _check(r, "maxsim_attention_backward")
     L = load()
     strides, q_offsets, k_offsets, sizes, scale = _attention_sizes(Q, K, V, q_offsets, k_offsets, scale)
     dQ, dK, dV = (torch.empty(x.shape, dtype=x.dtype, device=x.device) if g is None else g for g, x in ((dQ, Q), (dK, K), (dV, V)))
@@ -620,7 +643,7 @@ def maxsim_attention_backward(Q, K, V, out, lse, dout, q_offsets, k_offsets=None
     strides += _rows(dQ, "dQ", Q.shape, Q.dtype) + _rows(dK, "dK", K.shape, Q.dtype) + _rows(dV, "dV", K.shape, Q.dtype)
     _same(lse, "lse", Q.shape[:2], torch.float32)
     _same_device(Q, K=K, V=V, out=out, lse=lse, dout=dout, q_offsets=q_offsets, k_offsets=k_offsets, dQ=dQ, dK=dK, dV=dV)
-    with torch.cuda.device(Q.device):
+    with _gpu(Q):
         ws = _workspace(workspace, L.maxsim_attention_backward_workspace(*sizes), Q)
         rc = L.maxsim_attention_backward(Q.data_ptr(), K.data_ptr(), V.data_ptr(), out.data_ptr(), _dev(lse, "lse"), dout.data_ptr(), (ctypes.c_int64 * 16)(*strides),
                                          _dev(q_offsets, "q_offsets", torch.int32), _dev(k_offsets, "k_offsets", torch.int32), *sizes, _DTYPE[Q.dtype], int(bool(causal)),
@@ -633,8 +656,12 @@ def maxsim_attention_backward(Q, K, V, out, lse, dout, q_offsets, k_offsets=None
 def maxsim_clip_grad_norm(grads, max_norm, out=None, norm=None, workspace=None):
     """Scales gradients (a sequence of tensors, fp32, fp16 or bf16, mixed) by min(1, max_norm / (norm + 1e-6)), norm the 2-norm over all of
     them: in place, or into the tensors of out.  Returns the norm (fp32 [1], on the GPU: nothing waits for it)."""
-    L = load()
     grads = list(grads)
+    if _native is not None:
+        r = _native.clip_grad_norm(grads, max_norm, out if out is None else list(out), norm, workspace)
+        if r is not None:
+            return r if type(r) is not int else _check(r, "maxsim_clip_grad_norm")
+    L = load()
     out = grads if out is None else list(out)
     if not grads or len(out) != len(grads):
         raise MaxSimError("grads must hold a tensor at least, and out as many")
@@ -651,7 +678,7 @@ def maxsim_clip_grad_norm(grads, max_norm, out=None, norm=None, workspace=None):
         norm = torch.empty(1, dtype=torch.float32, device=grads[0].device)
     _same(norm, "norm", (1,), torch.float32)
     _same_device(grads[0], norm=norm)
-    with torch.cuda.device(grads[0].device):
+    with _gpu(grads[0]):
         ws = _workspace(workspace, L.maxsim_clip_workspace(n), norm)
         rc = L.maxsim_clip_grad_norm((ctypes.c_void_p * n)(*(g.data_ptr() for g in grads)), (ctypes.c_void_p * n)(*(o.data_ptr() for o in out)),
                                      (ctypes.c_int64 * n)(*(g.numel() for g in grads)), (ctypes.c_int32 * n)(*(_DTYPE[g.dtype] for g in grads)), n,

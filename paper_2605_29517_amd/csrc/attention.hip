@@ -14,6 +14,36 @@ constexpr int TILE = 64;                // keys per step
 constexpr float NO_MAXIMUM = -1.0e30f;  // of a row that has seen no key: finite, so that no difference of infinities arises
 constexpr float LAZY = 8.0f;            // the maximum may lag by this many powers of two: P <= 2^8, far from overflow in fp16
 
+// A column's result: O = o / sum and lse, or the same of a piece
+template <int DT, int NB> __device__ __forceinline__ void attn_write(const AttnParams &p, const f32x16 (&o)[NB], float top, float sum, int piece, int64_t token, int head, int h)
+{
+    const bool seen = sum > 0.0f;
+    const float by = seen ? 1.0f / sum : 0.0f;
+    const float lse = seen ? (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f : neg_inf();
+    const int64_t at = token * p.hq + head;
+    if (p.n_split > 1) {
+        float *part = p.part_o + ((int64_t)piece * p.q_tokens * p.hq + at) * p.d;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4)
+                if (32 * b + 2 * r + 4 * h < p.d)
+                    *reinterpret_cast<float4 *>(part + 32 * b + 2 * r + 4 * h) = make_float4(o[b][r] * by, o[b][r + 1] * by, o[b][r + 2] * by, o[b][r + 3] * by);
+        if (h == 0)
+            p.part_lse[(int64_t)piece * p.q_tokens * p.hq + at] = lse;
+        return;
+    }
+    char *row = p.O.p + token * p.O.token + head * p.O.head;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4)
+            if (32 * b + 2 * r + 4 * h < p.d)
+                attn_store4<DT>(row, 32 * b + 2 * r + 4 * h, o[b][r] * by, o[b][r + 1] * by, o[b][r + 2] * by, o[b][r + 3] * by);
+    if (p.lse && h == 0)
+        p.lse[at] = lse;
+}
+
 template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, 2) attn_fwd_kernel(AttnParams p)
 {
     constexpr int ROWS = NW * 32, U = DP / 16, NB = DP / 32;
@@ -139,56 +169,222 @@ template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, 2) 
     sum = attn_halves_sum(sum);
     if (row >= rows)
         return;
-    const bool seen = sum > 0.0f;
-    const float by = seen ? 1.0f / sum : 0.0f;
-    const float lse = seen ? (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f : neg_inf();
-    const int64_t at = (q.start + token) * p.hq + head;
-    if (p.n_split > 1) {
-        float *part = p.part_o + ((int64_t)piece * p.q_tokens * p.hq + at) * p.d;
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int r = 0; r < 16; r += 4)
-                if (32 * b + 2 * r + 4 * h < p.d)
-                    *reinterpret_cast<float4 *>(part + 32 * b + 2 * r + 4 * h) = make_float4(o[b][r] * by, o[b][r + 1] * by, o[b][r + 2] * by, o[b][r + 3] * by);
-        if (h == 0)
-            p.part_lse[(int64_t)piece * p.q_tokens * p.hq + at] = lse;
+    attn_write<DT>(p, o, top, sum, piece, q.start + token, head, h);
+}
+
+// The same for few rows per sequence (single tokens against kept keys): what counts is that keys and values stream at the memory's
+// rate. A wavefront owns all 32 rows of the workgroup and every NF-th tile of 32 keys of the piece, which it copies to a ring in
+// LDS of its own, RING tiles of K and of V ahead: nothing waits for another wavefront, and two workgroups keep 100 KB on their way to a compute
+// unit. The wavefronts' results are joined through LDS at the end.
+constexpr int NF = 2;
+template <int DT, int DP> __global__ void __launch_bounds__(NF * 64, 1) attn_few_kernel(AttnParams p)
+{
+    constexpr int U = DP / 16, NB = DP / 32;
+    constexpr int KEYS = 32, TILE_BYTES = KEYS * DP * 2, RING = 16384 / TILE_BYTES, LOADS = TILE_BYTES / 1024;
+    __shared__ __attribute__((aligned(16))) char lds[NF * RING * 2 * TILE_BYTES];
+
+    const int lane = threadIdx.x & 63, h = lane >> 5;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // The heads of a piece, whose rows lie side by side, run next to each other on one XCD
+    int v = xcd_grouped(blockIdx.x, gridDim.x);
+    const int hk = v % p.hkv;
+    v /= p.hkv;
+    const int piece = v % p.n_split, slot = v / p.n_split;
+
+    const int64_t i = attn_find_slot(p.q_off, p.b, p.q_tokens, p.pack, 32, slot);
+    const AttnSeq q = attn_seq(p.q_off, i, p.q_tokens), k = attn_seq(p.k_off, i, p.k_tokens);
+    const int64_t first = (int64_t)(slot - attn_first_slot(p.q_off, i, p.q_tokens, p.pack, 32)) * 32, rows = (int64_t)q.len * p.pack;
+    if (first < 0 || first >= rows)
         return;
+    const int64_t row = first + (lane & 31);
+    const int64_t row_ok = min(row, rows - 1);
+    const int token = (int)(row_ok / p.pack);
+    const int head = hk * p.pack + (int)(row_ok % p.pack);
+    const int ahead = k.len - q.len;
+    const int limit = p.causal ? max(0, min(k.len, token + ahead + 1)) : k.len;
+    const int wave_keys = __builtin_amdgcn_readlane(limit, 31), all_keys = __builtin_amdgcn_readfirstlane(limit);
+
+    const char *k_head = p.K.p + k.start * p.K.token + hk * p.K.head, *v_head = p.V.p + k.start * p.V.token + hk * p.V.head;
+    AttnCopy<DP, KEYS, 1> copy;
+    copy.init(0, lane, p.d);
+    const AttnRowRead<DP> k_read(lane);
+    const AttnColRead<DP> v_read(lane);
+
+    const int tiles = (wave_keys + KEYS - 1) / KEYS;
+    const int t0 = (int)((int64_t)tiles * piece / p.n_split) + w, t1 = (int)((int64_t)tiles * (piece + 1) / p.n_split);
+    const int n = t0 < t1 ? (t1 - t0 + NF - 1) / NF : 0; // tiles of this wavefront: t0, t0 + NF, ...
+    char *ring = lds + w * RING * 2 * TILE_BYTES;
+    auto issue_k = [&](int j) { copy.issue(k_head, p.K.token, (t0 + NF * j) * KEYS, k.len - 1, attn_lds(ring) + (j % RING) * 2 * TILE_BYTES, 0); };
+    auto issue_v = [&](int j) { copy.issue(v_head, p.V.token, (t0 + NF * j) * KEYS, k.len - 1, attn_lds(ring) + (j % RING) * 2 * TILE_BYTES + TILE_BYTES, 0); };
+    uint4 qf[U];
+    attn_load_row(p.Q.p + (q.start + token) * p.Q.token + head * p.Q.head, p.d, h, qf);
+    attn_have_row(p.d, h, qf);
+    for (int j = 0; j < RING && j < n; ++j) {
+        issue_k(j);
+        issue_v(j);
     }
-    char *o_row = p.O.p + (q.start + token) * p.O.token + head * p.O.head;
+
+    f32x16 o[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int r = 0; r < 16; r += 4)
-            if (32 * b + 2 * r + 4 * h < p.d)
-                attn_store4<DT>(o_row, 32 * b + 2 * r + 4 * h, o[b][r] * by, o[b][r + 1] * by, o[b][r + 2] * by, o[b][r + 3] * by);
-    if (p.lse && h == 0)
-        p.lse[at] = lse;
+        for (int r = 0; r < 16; ++r)
+            o[b][r] = 0.0f;
+    float top = NO_MAXIMUM, sum = 0.0f;
+    for (int j = 0; j < n; ++j) {
+        const char *kt = ring + (j % RING) * 2 * TILE_BYTES, *vt = kt + TILE_BYTES;
+        const int key0 = (t0 + NF * j) * KEYS;
+        // the newest copies may stay on their way: everything after this K, and after this V
+        if (j + RING - 1 < n)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"((2 * RING - 1) * LOADS) : "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        f32x16 s;
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            s[r] = 0.0f;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            attn_mma<DT>(k_read.get(kt, 0, u), qf[u], s);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); // K has been read
+        if (j + RING < n)
+            issue_k(j + RING);
+        if (key0 + KEYS > all_keys) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                s[r] = key0 + acc_row(r, h) < limit ? s[r] : neg_inf();
+        }
+        float m = s[0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r)
+            m = fmaxf(m, s[r]);
+        m = attn_halves_max(m) * p.scale_log2;
+        if (__builtin_amdgcn_ballot_w64(m > top + LAZY)) {
+            const float to = fmaxf(m, top), by = __builtin_amdgcn_exp2f(top - to);
+            top = to;
+            sum *= by;
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    o[b][r] *= by;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], p.scale_log2, -top));
+            sum += s[r];
+        }
+        if (j + RING < n)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"((2 * RING - 1) * LOADS) : "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const uint4 pf = attn_operand<DT>(s, x);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+                attn_mma<DT>(v_read.get(vt, nb, x), pf, o[nb]);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); // V has been read
+        if (j + RING < n)
+            issue_v(j + RING);
+    }
+    sum = attn_halves_sum(sum);
+
+    // the others' results into their rings, all of whose copies have been read
+    float *mine = reinterpret_cast<float *>(ring);
+    if (w > 0) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                mine[(b * 16 + r) * 64 + lane] = o[b][r];
+        mine[NB * 16 * 64 + lane] = top;
+        mine[NB * 16 * 64 + 64 + lane] = sum;
+    }
+    __syncthreads();
+    if (w > 0)
+        return;
+#pragma unroll
+    for (int x = 1; x < NF; ++x) {
+        const float *theirs = reinterpret_cast<const float *>(lds + x * RING * 2 * TILE_BYTES);
+        const float top2 = theirs[NB * 16 * 64 + lane], sum2 = theirs[NB * 16 * 64 + 64 + lane];
+        const float to = fmaxf(top, top2), by = __builtin_amdgcn_exp2f(top - to), by2 = __builtin_amdgcn_exp2f(top2 - to);
+        top = to;
+        sum = sum * by + sum2 * by2;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                o[b][r] = o[b][r] * by + theirs[(b * 16 + r) * 64 + lane] * by2;
+    }
+    if (row < rows)
+        attn_write<DT>(p, o, top, sum, piece, q.start + token, head, h);
 }
 
-// Joins the pieces: weights exp(lse_piece - lse), a thread per four entries of a row
-template <int DT> __global__ void __launch_bounds__(256) attn_join_kernel(AttnParams p)
+// Joins the pieces of a row: weights exp(lse_piece - lse). Eight lanes read 128 bytes of a piece; PIECES such groups take pieces of the
+// same row in turn (many pieces of few rows spread over the chip that way), the others of a workgroup take other rows.
+constexpr int MOST_PIECES = 256;
+template <int DT, int PIECES> __global__ void __launch_bounds__(256) attn_join_kernel(AttnParams p)
 {
     const int64_t n = p.q_tokens * p.hq;
-    const int per = p.d / 4;
-    const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x, at = x / per;
-    const int e = (int)(x % per) * 4;
-    if (at >= n)
-        return;
-    float top = neg_inf();
-    for (int s = 0; s < p.n_split; ++s)
-        top = fmaxf(top, p.part_lse[s * n + at]);
-    float sum = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (top > neg_inf())
-        for (int s = 0; s < p.n_split; ++s) {
-            const float by = __builtin_amdgcn_exp2f((p.part_lse[s * n + at] - top) * 1.44269504088896341f);
-            const float4 y = *reinterpret_cast<const float4 *>(p.part_o + (s * n + at) * p.d + e);
-            sum += by;
-            o[0] += by * y.x;
-            o[1] += by * y.y;
-            o[2] += by * y.z;
-            o[3] += by * y.w;
+    const int blocks = (p.d + 31) / 32;
+    const int group = threadIdx.x >> 3, g = group % PIECES;
+    const int64_t unit = (int64_t)blockIdx.x * (32 / PIECES) + group / PIECES;
+    const bool in = unit < n * blocks;
+    const int64_t at = in ? unit / blocks : 0;
+    const int e = min((int)(unit % blocks) * 32 + (int)(threadIdx.x & 7) * 4, p.d - 4); // (past the row's end: its last four again)
+    const float *lse = p.part_lse + at;
+
+    float top = NO_MAXIMUM, sum = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    auto add = [&](float by, int s) {
+        const float4 y = *reinterpret_cast<const float4 *>(p.part_o + (s * n + at) * p.d + e);
+        sum += by;
+        o[0] = __builtin_fmaf(by, y.x, o[0]);
+        o[1] = __builtin_fmaf(by, y.y, o[1]);
+        o[2] = __builtin_fmaf(by, y.z, o[2]);
+        o[3] = __builtin_fmaf(by, y.w, o[3]);
+    };
+    if constexpr (PIECES == 1) {
+        for (int s = 0; s < p.n_split; ++s)
+            top = fmaxf(top, lse[s * n]);
+        for (int s = 0; s < p.n_split; ++s)
+            add(__builtin_amdgcn_exp2f((lse[s * n] - top) * 1.44269504088896341f), s);
+    } else {
+        __shared__ float weight[MOST_PIECES], tops[4];
+        __shared__ float4 part[PIECES][8];
+        __shared__ float part_sum[PIECES];
+        const float mine = (int)threadIdx.x < p.n_split ? lse[threadIdx.x * n] : neg_inf();
+        top = fmaxf(top, mine);
+#pragma unroll
+        for (int m = 32; m; m >>= 1)
+            top = fmaxf(top, __shfl_xor(top, m, 64));
+        if ((threadIdx.x & 63) == 0)
+            tops[threadIdx.x >> 6] = top;
+        __syncthreads();
+        top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+        weight[threadIdx.x] = __builtin_amdgcn_exp2f((mine - top) * 1.44269504088896341f);
+        __syncthreads();
+#pragma unroll 8
+        for (int s = g; s < p.n_split; s += PIECES)
+            add(weight[s], s);
+        part[group][threadIdx.x & 7] = make_float4(o[0], o[1], o[2], o[3]);
+        part_sum[group] = sum;
+        __syncthreads();
+        if (g != 0)
+            return;
+#pragma unroll
+        for (int x = 1; x < PIECES; ++x) {
+            const float4 y = part[x][threadIdx.x & 7];
+            o[0] += y.x;
+            o[1] += y.y;
+            o[2] += y.z;
+            o[3] += y.w;
+            sum += part_sum[x];
         }
+    }
+    if (!in)
+        return;
     const float by = sum > 0.0f ? 1.0f / sum : 0.0f;
     const int64_t token = at / p.hq;
     const int head = (int)(at % p.hq);
@@ -199,20 +395,30 @@ template <int DT> __global__ void __launch_bounds__(256) attn_join_kernel(AttnPa
 
 struct AttnPlan {
     int pack, n_slots, n_split;
+    bool few; // attn_few_kernel
 };
 constexpr int NW = 4;
 
-AttnPlan attn_plan(int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, int hkv, int num_cu)
+AttnPlan attn_plan(int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, int hkv, int d, int num_cu)
 {
     AttnPlan x;
     x.pack = hq / hkv;
-    const int64_t slots = q_tokens * x.pack / (NW * 32) + b;
-    x.n_slots = (int)slots;
-    // pieces of the keys where the workgroups would leave compute units idle: as many as fill them twice, of at least four tiles of an average sequence
-    const int64_t busy = slots * hkv, mean = k_tokens / b / TILE;
-    int64_t split = busy >= num_cu ? 1 : (2 * num_cu + busy - 1) / busy;
-    split = std::min<int64_t>(split, mean / 4);
-    x.n_split = (int)std::max<int64_t>(1, std::min<int64_t>(split, 64));
+    x.few = q_tokens * x.pack <= 32 * b && k_tokens >= 256 * b;
+    x.n_slots = (int)(q_tokens * x.pack / (x.few ? 32 : NW * 32) + b);
+    // Pieces of the keys: an estimate of the time, in microseconds. A step of 64 keys of a workgroup takes 1.5 (few rows: 2.6, the
+    // memory's rate) while the chip is full (two workgroups to a compute unit), a workgroup's start 3; sequences differ in
+    // length, which costs some of a piece at the end; joining costs a launch and a round trip of fp32 results.
+    const double full = 2.0 * num_cu, tiles = std::max(1.0, (double)k_tokens / b / TILE), work = (double)x.n_slots * hkv;
+    const double step = (x.few ? 2.6 : 1.5) * d / 128, join = (double)q_tokens * hq * d * 8 / 4.0e6;
+    double best = 0;
+    x.n_split = 1;
+    for (int n = 1; n <= MOST_PIECES && n <= std::max(1.0, tiles / 4) && work * n < (1 << 24); n = n < 8 ? n + 1 : n + n / 4) {
+        const double time = (std::max(1.0, work * n / full) + 0.6) * (tiles / n * step + 3.0) + (n > 1 ? 4.0 + n * join : 0.0);
+        if (n == 1 || time < (x.n_split == 1 ? 0.85 : 1.0) * best) { // (one piece unless it costs clearly more)
+            best = time;
+            x.n_split = n;
+        }
+    }
     return x;
 }
 
@@ -220,13 +426,13 @@ AttnPlan attn_plan(int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, int hk
 
 int64_t attention_workspace(int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, int hkv, int d, int num_cu)
 {
-    const AttnPlan x = attn_plan(b, q_tokens, k_tokens, hq, hkv, num_cu);
+    const AttnPlan x = attn_plan(b, q_tokens, k_tokens, hq, hkv, d, num_cu);
     return x.n_split > 1 ? x.n_split * q_tokens * hq * (int64_t)(d + 1) * 4 : 0;
 }
 
 hipError_t attention_launch(AttnParams p, int dtype, void *workspace, int num_cu, hipStream_t stream)
 {
-    const AttnPlan x = attn_plan(p.b, p.q_tokens, p.k_tokens, p.hq, p.hkv, num_cu);
+    const AttnPlan x = attn_plan(p.b, p.q_tokens, p.k_tokens, p.hq, p.hkv, p.d, num_cu);
     p.pack = x.pack;
     p.n_slots = x.n_slots;
     p.n_split = x.n_split;
@@ -234,19 +440,34 @@ hipError_t attention_launch(AttnParams p, int dtype, void *workspace, int num_cu
     p.part_lse = p.part_o + (x.n_split > 1 ? x.n_split * p.q_tokens * p.hq * (int64_t)p.d : 0);
     const unsigned grid = (unsigned)(x.n_slots * p.hkv * x.n_split);
     const hipError_t e = attn_width(p.d, [&](auto dp) {
-        if (dtype == MAXSIM_F16)
-            attn_fwd_kernel<MAXSIM_F16, decltype(dp)::value, NW><<<grid, NW * 64, 0, stream>>>(p);
-        else
-            attn_fwd_kernel<MAXSIM_BF16, decltype(dp)::value, NW><<<grid, NW * 64, 0, stream>>>(p);
+        constexpr int DP = decltype(dp)::value;
+        if (x.few) {
+            if (dtype == MAXSIM_F16)
+                attn_few_kernel<MAXSIM_F16, DP><<<grid, NF * 64, 0, stream>>>(p);
+            else
+                attn_few_kernel<MAXSIM_BF16, DP><<<grid, NF * 64, 0, stream>>>(p);
+        } else if (dtype == MAXSIM_F16) {
+            attn_fwd_kernel<MAXSIM_F16, DP, NW><<<grid, NW * 64, 0, stream>>>(p);
+        } else {
+            attn_fwd_kernel<MAXSIM_BF16, DP, NW><<<grid, NW * 64, 0, stream>>>(p);
+        }
         return hipGetLastError();
     });
     if (e != hipSuccess || x.n_split == 1)
         return e;
-    const unsigned join = (unsigned)((p.q_tokens * p.hq * (p.d / 4) + 255) / 256);
-    if (dtype == MAXSIM_F16)
-        attn_join_kernel<MAXSIM_F16><<<join, 256, 0, stream>>>(p);
+    const int64_t units = p.q_tokens * p.hq * ((p.d + 31) / 32);
+    auto join = [&](auto pieces) {
+        constexpr int PIECES = decltype(pieces)::value;
+        const unsigned wgs = (unsigned)((units * PIECES + 31) / 32);
+        if (dtype == MAXSIM_F16)
+            attn_join_kernel<MAXSIM_F16, PIECES><<<wgs, 256, 0, stream>>>(p);
+        else
+            attn_join_kernel<MAXSIM_BF16, PIECES><<<wgs, 256, 0, stream>>>(p);
+    };
+    if (x.n_split <= 16)
+        join(std::integral_constant<int, 1>{});
     else
-        attn_join_kernel<MAXSIM_BF16><<<join, 256, 0, stream>>>(p);
+        join(std::integral_constant<int, 32>{});
     return hipGetLastError();
 }
 

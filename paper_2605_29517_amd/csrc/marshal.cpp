@@ -19,6 +19,8 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <climits>
+#include <cmath>
+#include <vector>
 
 #include "../../include/maxsim.h"
 
@@ -33,6 +35,13 @@ struct Entries {
     decltype(&maxsim_quantize_rows_i8) quantize;
     decltype(&maxsim_forward_i8) forward_i8;
     decltype(&maxsim_forward_i8_ragged) forward_i8_ragged;
+    decltype(&maxsim_rope) rope;
+    decltype(&maxsim_attention_workspace) attention_workspace;
+    decltype(&maxsim_attention) attention;
+    decltype(&maxsim_attention_backward_workspace) attention_backward_workspace;
+    decltype(&maxsim_attention_backward) attention_backward;
+    decltype(&maxsim_clip_workspace) clip_workspace;
+    decltype(&maxsim_clip_grad_norm) clip_grad_norm;
 } entry;
 
 // One call's arguments.  ok() after everything has been looked at: nothing was out of the ordinary.
@@ -51,18 +60,57 @@ public:
             ok_ = false;
             return none();
         }
-        if (device_ < 0) {
-            device_ = t->get_device();
-            ok_ = device_ == c10::hip::current_device();
-        }
-        ok_ = ok_ && t->get_device() == device_;
+        on_device(*t);
         return *t;
+    }
+    const at::Tensor &tensor(PyObject *o) // of any number of dimensions
+    {
+        const at::Tensor *t = ok_ ? plain(o) : nullptr;
+        return t ? tensor(o, (int)t->dim()) : (ok_ = false, none());
     }
     const at::Tensor &tensor(PyObject *o, at::IntArrayRef shape, at::ScalarType type)
     {
         const at::Tensor &t = tensor(o, (int)shape.size());
         ok_ = ok_ && t.scalar_type() == type && t.sizes() == shape;
         return ok_ ? t : none();
+    }
+    // A packed tensor [tokens, heads, d], which may be a view with rows of stride 1, and its two strides
+    const at::Tensor &rows(PyObject *o, int64_t *strides)
+    {
+        const at::Tensor *t = ok_ ? plain(o) : nullptr;
+        if (!t || t->dim() != 3 || t->numel() == 0 || (t->size(2) > 1 && t->stride(2) != 1)) {
+            ok_ = false;
+            return none();
+        }
+        on_device(*t);
+        strides[0] = t->size(0) > 1 ? t->stride(0) : t->size(2);
+        strides[1] = t->size(1) > 1 ? t->stride(1) : t->size(2);
+        return *t;
+    }
+    const at::Tensor &rows(PyObject *o, int64_t *strides, const at::Tensor &like)
+    {
+        const at::Tensor &t = rows(o, strides);
+        ok_ = ok_ && t.scalar_type() == like.scalar_type() && t.sizes() == like.sizes();
+        return ok_ ? t : none();
+    }
+    at::Tensor output_rows(PyObject *o, int64_t *strides, const at::Tensor &like)
+    {
+        if (o != Py_None)
+            return rows(o, strides, like);
+        if (!ok_)
+            return at::Tensor();
+        strides[0] = like.size(0) > 1 ? like.size(1) * like.size(2) : like.size(2);
+        strides[1] = like.size(2);
+        return at::empty(like.sizes(), at::TensorOptions().dtype(like.scalar_type()).device(at::kCUDA, device_));
+    }
+    at::Tensor workspace(PyObject *o, int64_t bytes) // the caller's, of any length, or a new one
+    {
+        if (o != Py_None) {
+            const at::Tensor &t = tensor(o, 1);
+            ok_ = ok_ && t.scalar_type() == at::kByte;
+            return ok_ ? t : none();
+        }
+        return ok_ && bytes ? at::empty({bytes}, at::TensorOptions().dtype(at::kByte).device(at::kCUDA, device_)) : at::Tensor();
     }
     // The caller's output or, for None, a new one
     at::Tensor output(PyObject *o, at::IntArrayRef shape, at::ScalarType type)
@@ -88,6 +136,14 @@ public:
     void *stream() const { return c10::hip::getCurrentHIPStream((c10::DeviceIndex)device_).stream(); }
 
 private:
+    void on_device(const at::Tensor &t)
+    {
+        if (device_ < 0) {
+            device_ = t.get_device();
+            ok_ = device_ == c10::hip::current_device();
+        }
+        ok_ = ok_ && t.get_device() == device_;
+    }
     static const at::Tensor &none() // (not looked at: ok() is false)
     {
         static const at::Tensor t;
@@ -338,12 +394,192 @@ PyObject *forward_i8_ragged(PyObject *, PyObject *const *a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// A flag as Python has it
+bool flag(PyObject *o, Call &c)
+{
+    const int x = PyBool_Check(o) ? o == Py_True : -1;
+    c.require(x >= 0);
+    return x > 0;
+}
+float real(PyObject *o, Call &c)
+{
+    c.require(PyFloat_CheckExact(o));
+    return c.ok() ? (float)PyFloat_AS_DOUBLE(o) : 0.0f;
+}
+
+// (X, freqs, positions, offsets, interleaved, inverse, scale, out)
+PyObject *rope(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    ARGUMENTS(8)
+    Call c(a[0]);
+    int64_t xs[2], ys[2];
+    const at::Tensor &X = c.rows(a[0], xs), &freqs = c.tensor(a[1], 1);
+    const maxsim_dtype dt = c.dtype(X);
+    c.require(c.ok() && freqs.scalar_type() == at::kFloat && freqs.size(0) >= 1 && 2 * freqs.size(0) <= X.size(2));
+    const bool neighbours = flag(a[4], c), inverse = flag(a[5], c);
+    const float scale = real(a[6], c);
+    if (!c.ok())
+        Py_RETURN_NONE;
+    const int32_t *positions = nullptr, *offsets = nullptr;
+    int64_t b = 0;
+    if (a[2] != Py_None) {
+        const at::Tensor &p = c.tensor(a[2], {X.size(0)}, at::kInt);
+        positions = c.ok() ? at_ptr<int32_t>(p) : nullptr;
+    } else if (a[3] != Py_None) {
+        const at::Tensor &o = c.tensor(a[3], 1);
+        c.require(c.ok() && o.scalar_type() == at::kInt && o.size(0) >= 2);
+        if (!c.ok())
+            Py_RETURN_NONE;
+        offsets = at_ptr<int32_t>(o);
+        b = o.size(0) - 1;
+    }
+    const int heads = c.size(X.size(1)), d = c.size(X.size(2));
+    const at::Tensor Y = c.output_rows(a[7], ys, X);
+    if (!c.ok())
+        Py_RETURN_NONE;
+    const int rc = without_gil([&] {
+        return entry.rope(in(X), X.size(0), heads, d, xs[0], xs[1], dt, at_ptr<float>(freqs), 2 * (int)freqs.size(0), positions, offsets, b, scale, neighbours, inverse,
+                          Y.data_ptr(), ys[0], ys[1], c.stream());
+    });
+    return rc != 0 ? PyLong_FromLong(rc) : give(a[7], Y);
+    END_HANDLE_TH_ERRORS
+}
+
+// What both directions of attention look at first
+struct Attention {
+    int64_t strides[16];
+    const int32_t *q_off, *k_off;
+    int64_t b, tq, tk;
+    int hq, hkv, d;
+    maxsim_dtype dt;
+    float scale;
+
+    void look(Call &c, const at::Tensor &Q, const at::Tensor &K, const at::Tensor &V, PyObject *q_offsets, PyObject *k_offsets, PyObject *scale_)
+    {
+        dt = c.dtype(Q);
+        c.require(c.ok() && dt != MAXSIM_F32 && K.scalar_type() == Q.scalar_type() && V.scalar_type() == Q.scalar_type() && K.sizes() == V.sizes() && K.size(2) == Q.size(2) &&
+                  Q.size(1) % K.size(1) == 0);
+        if (!c.ok())
+            return;
+        tq = Q.size(0), tk = K.size(0);
+        hq = c.size(Q.size(1)), hkv = c.size(K.size(1)), d = c.size(Q.size(2));
+        const at::Tensor &qo = c.tensor(q_offsets, 1);
+        c.require(c.ok() && qo.scalar_type() == at::kInt && qo.size(0) >= 2 && ((k_offsets != Py_None && k_offsets != q_offsets) || tq == tk));
+        if (!c.ok())
+            return;
+        q_off = k_off = at_ptr<int32_t>(qo);
+        b = qo.size(0) - 1;
+        if (k_offsets != Py_None) {
+            const at::Tensor &ko = c.tensor(k_offsets, {b + 1}, at::kInt);
+            k_off = c.ok() ? at_ptr<int32_t>(ko) : nullptr;
+        }
+        scale = scale_ == Py_None ? (float)std::pow((double)d, -0.5) : real(scale_, c);
+    }
+};
+
+// (Q, K, V, q_offsets, k_offsets, causal, scale, out, lse, workspace)
+PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    ARGUMENTS(10)
+    Call c(a[0]);
+    Attention x;
+    const at::Tensor &Q = c.rows(a[0], x.strides), &K = c.rows(a[1], x.strides + 2), &V = c.rows(a[2], x.strides + 4);
+    x.look(c, Q, K, V, a[3], a[4], a[6]);
+    const bool causal = flag(a[5], c);
+    if (!c.ok())
+        Py_RETURN_NONE;
+    const at::Tensor O = c.output_rows(a[7], x.strides + 6, Q), lse = c.output(a[8], {x.tq, x.hq}, at::kFloat);
+    const at::Tensor ws = c.workspace(a[9], c.ok() ? entry.attention_workspace(x.b, x.tq, x.tk, x.hq, x.hkv, x.d) : 0);
+    if (!c.ok())
+        Py_RETURN_NONE;
+    const int rc = without_gil([&] {
+        return entry.attention(in(Q), in(K), in(V), x.strides, x.q_off, x.k_off, x.b, x.tq, x.tk, x.hq, x.hkv, x.d, x.dt, causal, x.scale, O.data_ptr(), at_ptr<float>(lse),
+                               ws.defined() ? ws.data_ptr() : nullptr, ws.defined() ? ws.numel() : 0, c.stream());
+    });
+    return rc != 0 ? PyLong_FromLong(rc) : give2(a[7], O, a[8], lse);
+    END_HANDLE_TH_ERRORS
+}
+
+// (Q, K, V, out, lse, dout, q_offsets, k_offsets, causal, scale, dQ, dK, dV, workspace)
+PyObject *attention_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    ARGUMENTS(14)
+    Call c(a[0]);
+    Attention x;
+    const at::Tensor &Q = c.rows(a[0], x.strides), &K = c.rows(a[1], x.strides + 2), &V = c.rows(a[2], x.strides + 4);
+    x.look(c, Q, K, V, a[6], a[7], a[9]);
+    const bool causal = flag(a[8], c);
+    if (!c.ok())
+        Py_RETURN_NONE;
+    const at::Tensor &O = c.rows(a[3], x.strides + 6, Q), &lse = c.tensor(a[4], {x.tq, x.hq}, at::kFloat), &dO = c.rows(a[5], x.strides + 8, Q);
+    const at::Tensor dQ = c.output_rows(a[10], x.strides + 10, Q), dK = c.output_rows(a[11], x.strides + 12, K), dV = c.output_rows(a[12], x.strides + 14, V);
+    const at::Tensor ws = c.workspace(a[13], c.ok() ? entry.attention_backward_workspace(x.b, x.tq, x.tk, x.hq, x.hkv, x.d) : 0);
+    if (!c.ok())
+        Py_RETURN_NONE;
+    const int rc = without_gil([&] {
+        return entry.attention_backward(in(Q), in(K), in(V), in(O), at_ptr<float>(lse), in(dO), x.strides, x.q_off, x.k_off, x.b, x.tq, x.tk, x.hq, x.hkv, x.d, x.dt, causal,
+                                        x.scale, dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), ws.defined() ? ws.data_ptr() : nullptr, ws.defined() ? ws.numel() : 0, c.stream());
+    });
+    if (rc != 0)
+        return PyLong_FromLong(rc);
+    PyObject *two = give2(a[10], dQ, a[11], dK), *third = two ? give(a[12], dV) : nullptr;
+    PyObject *r = third ? PyTuple_Pack(3, PyTuple_GET_ITEM(two, 0), PyTuple_GET_ITEM(two, 1), third) : nullptr;
+    Py_XDECREF(two);
+    Py_XDECREF(third);
+    return r;
+    END_HANDLE_TH_ERRORS
+}
+
+// (grads, max_norm, out, norm, workspace): grads and out (or None) lists
+PyObject *clip_grad_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    ARGUMENTS(5)
+    if (!PyList_CheckExact(a[0]) || !(a[2] == Py_None || PyList_CheckExact(a[2])))
+        Py_RETURN_NONE;
+    const Py_ssize_t count = PyList_GET_SIZE(a[0]);
+    if (count < 1 || count > INT_MAX || (a[2] != Py_None && PyList_GET_SIZE(a[2]) != count))
+        Py_RETURN_NONE;
+    Call c(PyList_GET_ITEM(a[0], 0));
+    std::vector<const void *> g(count);
+    std::vector<void *> out(count);
+    std::vector<int64_t> numel(count);
+    std::vector<int32_t> dtype(count);
+    for (Py_ssize_t i = 0; i < count; ++i) {
+        const at::Tensor &t = c.tensor(PyList_GET_ITEM(a[0], i));
+        dtype[i] = c.dtype(t);
+        if (!c.ok())
+            Py_RETURN_NONE;
+        g[i] = out[i] = t.data_ptr();
+        numel[i] = t.numel();
+        if (a[2] != Py_None) {
+            const at::Tensor &o = c.tensor(PyList_GET_ITEM(a[2], i));
+            c.require(c.ok() && o.scalar_type() == t.scalar_type() && o.sizes() == t.sizes());
+            if (!c.ok())
+                Py_RETURN_NONE;
+            out[i] = o.data_ptr();
+        }
+    }
+    const float max_norm = real(a[1], c);
+    const at::Tensor norm = c.output(a[3], {1}, at::kFloat), ws = c.workspace(a[4], c.ok() ? entry.clip_workspace((int)count) : 0);
+    if (!c.ok())
+        Py_RETURN_NONE;
+    const int rc = without_gil([&] {
+        return entry.clip_grad_norm(g.data(), out.data(), numel.data(), dtype.data(), (int)count, max_norm, at_ptr<float>(norm), ws.data_ptr(), ws.numel(), c.stream());
+    });
+    return rc != 0 ? PyLong_FromLong(rc) : give(a[3], norm);
+    END_HANDLE_TH_ERRORS
+}
+
 // The addresses of the entry points in the library that binding.py has loaded, in the order of Entries
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
-    ARGUMENTS(8)
-    void *p[8];
-    for (int i = 0; i < 8; ++i) {
+    ARGUMENTS(15)
+    void *p[15];
+    for (int i = 0; i < 15; ++i) {
         p[i] = PyLong_AsVoidPtr(a[i]);
         if (PyErr_Occurred())
             return nullptr;
@@ -357,12 +593,20 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
     entry.quantize = reinterpret_cast<decltype(entry.quantize)>(p[i++]);
     entry.forward_i8 = reinterpret_cast<decltype(entry.forward_i8)>(p[i++]);
     entry.forward_i8_ragged = reinterpret_cast<decltype(entry.forward_i8_ragged)>(p[i++]);
+    entry.rope = reinterpret_cast<decltype(entry.rope)>(p[i++]);
+    entry.attention_workspace = reinterpret_cast<decltype(entry.attention_workspace)>(p[i++]);
+    entry.attention = reinterpret_cast<decltype(entry.attention)>(p[i++]);
+    entry.attention_backward_workspace = reinterpret_cast<decltype(entry.attention_backward_workspace)>(p[i++]);
+    entry.attention_backward = reinterpret_cast<decltype(entry.attention_backward)>(p[i++]);
+    entry.clip_workspace = reinterpret_cast<decltype(entry.clip_workspace)>(p[i++]);
+    entry.clip_grad_norm = reinterpret_cast<decltype(entry.clip_grad_norm)>(p[i++]);
     Py_RETURN_NONE;
 }
 
 #define METHOD(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(NAME)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(bind),     METHOD(forward),    METHOD(forward_ragged),    METHOD(backward), METHOD(backward_ragged), METHOD(ce_grad),
-                         METHOD(quantize), METHOD(forward_i8), METHOD(forward_i8_ragged), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(quantize), METHOD(forward_i8), METHOD(forward_i8_ragged), METHOD(rope), METHOD(attention), METHOD(attention_backward),
+                         METHOD(clip_grad_norm), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 } // namespace
