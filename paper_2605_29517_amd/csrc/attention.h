@@ -82,9 +82,12 @@ template <int DP> struct AttnTile {
 // loads into LDS before every LDS read that it cannot tell from their destination, which is the other buffer here; attn_arrive waits
 // for them. No vector register is written; m0, which names the destination, has no other user in these kernels.
 __device__ __forceinline__ uint32_t attn_lds(const void *p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p; }
-__device__ __forceinline__ void attn_load_lds16(const char *base, uint32_t offset, uint32_t dst)
+template <bool ONCE> __device__ __forceinline__ void attn_load_lds16(const char *base, uint32_t offset, uint32_t dst)
 {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(dst) : "memory");
+    if constexpr (ONCE) // read once: the caches need not keep it
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(offset), "s"(base), "s"(dst) : "memory");
+    else
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(dst) : "memory");
 }
 __device__ __forceinline__ void attn_load_lds4(const void *base, uint32_t offset, uint32_t dst)
 {
@@ -93,7 +96,7 @@ __device__ __forceinline__ void attn_load_lds4(const void *base, uint32_t offset
 
 // Copies ROWS consecutive rows of one head to LDS, NW wavefronts together; a wavefront's instruction fills 1 KB. Rows past `last`
 // are the last one's copies and chunks past the row's end are the last chunk's: what is masked later is finite, and of this sequence.
-template <int DP, int ROWS, int NW> struct AttnCopy {
+template <int DP, int ROWS, int NW, bool ONCE = false> struct AttnCopy {
     static constexpr int CH = DP / 8, N = ROWS * CH / 64, PER = (N + NW - 1) / NW;
     static constexpr bool EVEN = NW * 64 % (8 * CH) == 0; // a lane's rows are STEP apart, its chunk is the same in all of them
     static constexpr int STEP = NW * 64 / CH, HELD = EVEN ? 1 : PER;
@@ -118,7 +121,7 @@ template <int DP, int ROWS, int NW> struct AttnCopy {
             if (N % NW != 0 && w + NW * i >= N)
                 break;
             const int r = EVEN ? row[0] + STEP * i : row[EVEN ? 0 : i];
-            attn_load_lds16(base, (uint32_t)min(r, last - row0) * token_stride + at[EVEN ? 0 : i], tile + (w + NW * i) * 1024);
+            attn_load_lds16<ONCE>(base, (uint32_t)min(r, last - row0) * token_stride + at[EVEN ? 0 : i], tile + (w + NW * i) * 1024);
         }
     }
 };

@@ -205,7 +205,7 @@ template <int DT, int DP> __global__ void __launch_bounds__(NF * 64, 1) attn_few
     const int wave_keys = __builtin_amdgcn_readlane(limit, 31), all_keys = __builtin_amdgcn_readfirstlane(limit);
 
     const char *k_head = p.K.p + k.start * p.K.token + hk * p.K.head, *v_head = p.V.p + k.start * p.V.token + hk * p.V.head;
-    AttnCopy<DP, KEYS, 1> copy;
+    AttnCopy<DP, KEYS, 1, true> copy;
     copy.init(0, lane, p.d);
     const AttnRowRead<DP> k_read(lane);
     const AttnColRead<DP> v_read(lane);
@@ -405,15 +405,15 @@ AttnPlan attn_plan(int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, int hk
     x.pack = hq / hkv;
     x.few = q_tokens * x.pack <= 32 * b && k_tokens >= 256 * b;
     x.n_slots = (int)(q_tokens * x.pack / (x.few ? 32 : NW * 32) + b);
-    // Pieces of the keys: an estimate of the time, in microseconds. A step of 64 keys of a workgroup takes 1.5 (few rows: 2.6, the
-    // memory's rate) while the chip is full (two workgroups to a compute unit), a workgroup's start 3; sequences differ in
+    // Pieces of the keys: an estimate of the time, in microseconds. A step of 64 keys of a workgroup takes 1.5 (few rows: 2.2, the
+    // memory's rate) while the chip is full (two workgroups to a compute unit), a workgroup's start 5; sequences differ in
     // length, which costs some of a piece at the end; joining costs a launch and a round trip of fp32 results.
     const double full = 2.0 * num_cu, tiles = std::max(1.0, (double)k_tokens / b / TILE), work = (double)x.n_slots * hkv;
-    const double step = (x.few ? 2.6 : 1.5) * d / 128, join = (double)q_tokens * hq * d * 8 / 4.0e6;
+    const double step = (x.few ? 2.2 : 1.5) * d / 128, join = (double)q_tokens * hq * d * 8 / 4.0e6;
     double best = 0;
     x.n_split = 1;
     for (int n = 1; n <= MOST_PIECES && n <= std::max(1.0, tiles / 4) && work * n < (1 << 24); n = n < 8 ? n + 1 : n + n / 4) {
-        const double time = (std::max(1.0, work * n / full) + 0.6) * (tiles / n * step + 3.0) + (n > 1 ? 4.0 + n * join : 0.0);
+        const double time = (std::max(1.0, work * n / full) + 0.6) * (tiles / n * step + 5.0) + (n > 1 ? 4.0 + n * join : 0.0);
         if (n == 1 || time < (x.n_split == 1 ? 0.85 : 1.0) * best) { // (one piece unless it costs clearly more)
             best = time;
             x.n_split = n;
