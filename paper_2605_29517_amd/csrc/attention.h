@@ -35,28 +35,6 @@ struct AttnParams {
     float scale, scale_log2; // scale_log2 = scale * log2(e)
 };
 
-// Whether a sequence has tile t of `rows` rows is not known to the host, which has no lengths. Sequence i gets the tile slots
-// [first(i), first(i + 1)), first(i) = floor(offset_i / rows) + i: always as many as it needs and at most one too many, so that the
-// launch is tokens / rows + b tiles and a slot finds its sequence by a search over the offsets. `mul`: rows per token.
-__device__ __forceinline__ int64_t attn_first_slot(const int32_t *off, int64_t i, int64_t tokens, int mul, int rows)
-{
-    return clamp_offset(off[i], 0, tokens) * mul / rows + i;
-}
-// The sequence of a slot: the last i with first(i) <= slot (all lanes active, slot uniform)
-__device__ __forceinline__ int64_t attn_find_slot(const int32_t *off, int64_t b, int64_t tokens, int mul, int rows, int64_t slot)
-{
-    OffsetSearch s; // the first i in [0, b) with first(i) > slot, b if there is none
-    s.begin(b - 1);
-    while (s.open()) {
-        const uint32_t at = s.probe(threadIdx.x & 63);
-        const bool in = at < s.end;
-        const int64_t first = attn_first_slot(off, in ? at : 0u, tokens, mul, rows);
-        s.narrow(__builtin_amdgcn_ballot_w64(in && first <= slot));
-    }
-    const uint32_t i = __builtin_amdgcn_readfirstlane(s.lo);
-    return i ? (int64_t)i - 1 : 0;
-}
-
 // Rows of one sequence
 struct AttnSeq {
     int64_t start;
@@ -68,13 +46,54 @@ __device__ __forceinline__ AttnSeq attn_seq(const int32_t *off, int64_t i, int64
     return {s, (int)(e - s)};
 }
 
-// A tile of rows in LDS: CH chunks of 16 bytes a row, chunk c of row r at position c ^ swizzle(r). A read of one chunk of eight
-// consecutive rows (the operand as it lies) and a transposing read of 32 bytes of four rows both meet every bank once.
+// Whether a sequence has tile t of `rows` rows is not known to the host, which has no lengths. Sequence i gets the tile slots
+// [first(i), first(i + 1)), first(i) = floor(offset_i * mul / rows) + i, mul the rows of a token: always as many as it needs and at most
+// one too many, so that the launch is tokens * mul / rows + b tiles and a slot finds its sequence, the last i with first(i) <= slot, by a
+// search over the offsets. Each step of a search is a round trip to memory before anything else can start: the first looks at the 64
+// sequences around the place that equal lengths would give, and mostly ends it (always up to 63 sequences). All lanes active, slot uniform.
+struct AttnPlace {
+    int64_t i, first; // the sequence, and its first slot
+    AttnSeq s;
+};
+__device__ __forceinline__ AttnPlace attn_find_slot(const int32_t *off, int64_t b, int64_t tokens, int mul, int rows, int slot, int n_slots)
+{
+    const int64_t guess = (int64_t)((float)slot * (float)b / (float)n_slots) - 32;
+    const int64_t lo = guess > b - 63 ? (b > 63 ? b - 63 : 0) : guess < 0 ? 0 : guess;
+    const int64_t at = lo + (threadIdx.x & 63);
+    const int64_t v = clamp_offset(off[at < b ? at : b], 0, tokens);
+    const uint64_t below = __builtin_amdgcn_ballot_w64(at < b && v * mul / rows + at <= slot);
+    const int n = __builtin_popcountll(below);
+    AttnPlace x;
+    if (n > 0 && n < 64) {
+        x.i = lo + n - 1;
+        x.s.start = (uint32_t)__builtin_amdgcn_readlane((int)v, n - 1);
+        const int64_t end = (uint32_t)__builtin_amdgcn_readlane((int)v, n);
+        x.s.len = (int)(end > x.s.start ? end - x.s.start : 0);
+    } else {
+        OffsetSearch s; // the first i in [0, b) with first(i) > slot, b if there is none
+        s.begin(b - 1);
+        while (s.open()) {
+            const uint32_t p = s.probe(threadIdx.x & 63);
+            const bool in = p < s.end;
+            const int64_t first = clamp_offset(off[in ? p : 0u], 0, tokens) * mul / rows + p;
+            s.narrow(__builtin_amdgcn_ballot_w64(in && first <= slot));
+        }
+        const uint32_t i = __builtin_amdgcn_readfirstlane(s.lo);
+        x.i = i ? (int64_t)i - 1 : 0;
+        x.s = attn_seq(off, x.i, tokens);
+    }
+    x.first = x.s.start * mul / rows + x.i;
+    return x;
+}
+
+// A tile of rows in LDS: CH chunks of 16 bytes a row, chunk c of row r at position c ^ swizzle(r). LDS serves 256 bytes at a time, 64
+// banks of 4: a read of one chunk of sixteen consecutive rows (the operand as it lies) and a transposing read of 64 bytes of four
+// rows (both halves of it) then both meet every bank once.
 template <int DP> struct AttnTile {
     static constexpr int CH = DP / 8, ROW = DP * 2;
     static __device__ __forceinline__ constexpr int swizzle(int r)
     {
-        return CH % 8 == 0 ? ((r & 3) << 1) | ((r >> 2) & 1) : (((r >> 1) & 1) << 1) | ((r >> 2) & 1);
+        return (CH == 16 ? (r & 3) << 2 : CH == 8 ? ((r >> 1) & 1) << 2 : 0) | ((r >> 2) & 3);
     }
 };
 
@@ -98,7 +117,7 @@ __device__ __forceinline__ void attn_load_lds4(const void *base, uint32_t offset
 // are the last one's copies and chunks past the row's end are the last chunk's: what is masked later is finite, and of this sequence.
 template <int DP, int ROWS, int NW, bool ONCE = false> struct AttnCopy {
     static constexpr int CH = DP / 8, N = ROWS * CH / 64, PER = (N + NW - 1) / NW;
-    static constexpr bool EVEN = NW * 64 % (8 * CH) == 0; // a lane's rows are STEP apart, its chunk is the same in all of them
+    static constexpr bool EVEN = NW * 64 % (16 * CH) == 0; // a lane's rows are STEP apart, its chunk is the same in all of them
     static constexpr int STEP = NW * 64 / CH, HELD = EVEN ? 1 : PER;
     int row[HELD]; // this lane's row, and the byte of its chunk in it, per instruction
     uint32_t at[HELD];
@@ -185,9 +204,10 @@ template <int DP> struct AttnColRead {
     {
         typedef short s16x4 __attribute__((ext_vector_type(4)));
         typedef __attribute__((address_space(3))) s16x4 *lds_ptr;
-        const char *at = tile + s * 16 * AttnTile<DP>::ROW + base + (((4 * block) ^ chunk) << 4);
-        const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)at));
-        const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + 8 * AttnTile<DP>::ROW)));
+        const char *at = tile + s * 16 * AttnTile<DP>::ROW + base;
+        // (eight rows on, the swizzle differs in bit 1)
+        const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + (((4 * block) ^ chunk) << 4))));
+        const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + 8 * AttnTile<DP>::ROW + (((4 * block + 2) ^ chunk) << 4))));
         return make_uint4(x.x, x.y, y.x, y.y);
     }
 };

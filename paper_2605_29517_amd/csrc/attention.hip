@@ -44,9 +44,10 @@ template <int DT, int NB> __device__ __forceinline__ void attn_write(const AttnP
         p.lse[at] = lse;
 }
 
-template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, 2) attn_fwd_kernel(AttnParams p)
+template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, DP > 64 ? 2 : 4) attn_fwd_kernel(AttnParams p)
 {
     constexpr int ROWS = NW * 32, U = DP / 16, NB = DP / 32;
+    constexpr int B = DP > 64 ? 2 : 1;
     constexpr int TILE_BYTES = TILE * DP * 2;
     __shared__ __attribute__((aligned(16))) char lds[4 * TILE_BYTES]; // two of K, two of V
 
@@ -59,9 +60,9 @@ template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, 2) 
     v /= p.n_split;
     const int slot = p.n_slots - 1 - v % p.n_slots, hk = v / p.n_slots;
 
-    const int64_t i = attn_find_slot(p.q_off, p.b, p.q_tokens, p.pack, ROWS, slot);
-    const AttnSeq q = attn_seq(p.q_off, i, p.q_tokens), k = attn_seq(p.k_off, i, p.k_tokens);
-    const int64_t first = (int64_t)(slot - attn_first_slot(p.q_off, i, p.q_tokens, p.pack, ROWS)) * ROWS, rows = (int64_t)q.len * p.pack;
+    const AttnPlace place = attn_find_slot(p.q_off, p.b, p.q_tokens, p.pack, ROWS, slot, p.n_slots);
+    const AttnSeq q = place.s, k = p.k_off == p.q_off ? q : attn_seq(p.k_off, place.i, p.k_tokens);
+    const int64_t first = (slot - place.first) * ROWS, rows = (int64_t)q.len * p.pack;
     if (first < 0 || first >= rows)
         return;
 
@@ -75,7 +76,7 @@ template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, 2) 
     // keys that the rows of the workgroup and of the wavefront see, and those that all rows of the wavefront see
     const int64_t wg_last = min(first + ROWS, rows) - 1;
     const int wg_keys = p.causal ? max(0, min(k.len, (int)(wg_last / p.pack) + ahead + 1)) : k.len;
-    const int wave_keys = __builtin_amdgcn_readlane(limit, 31), all_keys = __builtin_amdgcn_readfirstlane(limit);
+    const int wave_keys = first + w * 32 < rows ? __builtin_amdgcn_readlane(limit, 31) : 0, all_keys = __builtin_amdgcn_readfirstlane(limit);
 
     uint4 qf[U];
     const char *q_row = p.Q.p + (q.start + token) * p.Q.token + head * p.Q.head;
@@ -102,20 +103,11 @@ template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, 2) 
         copy.issue(k_head, p.K.token, t * TILE, k.len - 1, to, w);
         copy.issue(v_head, p.V.token, t * TILE, k.len - 1, to + TILE_BYTES, w);
     };
-    if (t0 < t1)
-        issue(t0);
-    attn_have_row(p.d, h, qf);
-    for (int t = t0; t < t1; ++t) {
-        attn_arrive();
-        if (t + 1 < t1)
-            issue(t + 1);
-        const char *kt = lds + (t & 1) * 2 * TILE_BYTES, *vt = kt + TILE_BYTES;
-        const int key0 = t * TILE;
-        if (key0 >= wave_keys)
-            continue;
-        f32x16 s[2];
+    // B blocks of 32 keys of a tile; key0: the first of them
+    auto step = [&](const char *kt, const char *vt, int key0) {
+        f32x16 s[B];
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < B; ++b) {
 #pragma unroll
             for (int r = 0; r < 16; ++r)
                 s[b][r] = 0.0f;
@@ -123,16 +115,16 @@ template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, 2) 
             for (int u = 0; u < U; ++u)
                 attn_mma<DT>(k_read.get(kt, b, u), qf[u], s[b]);
         }
-        if (key0 + TILE > all_keys) {
+        if (key0 + 32 * B > all_keys) {
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
+            for (int b = 0; b < B; ++b)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     s[b][r] = key0 + 32 * b + acc_row(r, h) < limit ? s[b][r] : neg_inf();
         }
         float m = s[0][0];
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < B; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r)
                 m = fmaxf(m, s[b][r]);
@@ -149,14 +141,14 @@ template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, 2) 
                     o[b][r] *= by;
         }
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < B; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 s[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], p.scale_log2, -top));
                 sum += s[b][r];
             }
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < B; ++b)
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 const uint4 pf = attn_operand<DT>(s[b], x);
@@ -164,6 +156,22 @@ template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, 2) 
                 for (int nb = 0; nb < NB; ++nb)
                     attn_mma<DT>(v_read.get(vt, nb, 2 * b + x), pf, o[nb]);
             }
+    };
+    if (t0 < t1)
+        issue(t0);
+    attn_have_row(p.d, h, qf);
+    for (int t = t0; t < t1; ++t) {
+        attn_arrive();
+        if (t + 1 < t1)
+            issue(t + 1);
+        const char *kt = lds + (t & 1) * 2 * TILE_BYTES, *vt = kt + TILE_BYTES;
+        const int key0 = t * TILE;
+        if (key0 >= wave_keys)
+            continue;
+#pragma unroll
+        for (int b = 0; b < TILE / 32; b += B)
+            if (b == 0 || key0 + 32 * b < wave_keys)
+                step(kt + b * 32 * DP * 2, vt + b * 32 * DP * 2, key0 + 32 * b);
     }
 
     sum = attn_halves_sum(sum);
@@ -191,9 +199,9 @@ template <int DT, int DP> __global__ void __launch_bounds__(NF * 64, 1) attn_few
     v /= p.hkv;
     const int piece = v % p.n_split, slot = v / p.n_split;
 
-    const int64_t i = attn_find_slot(p.q_off, p.b, p.q_tokens, p.pack, 32, slot);
-    const AttnSeq q = attn_seq(p.q_off, i, p.q_tokens), k = attn_seq(p.k_off, i, p.k_tokens);
-    const int64_t first = (int64_t)(slot - attn_first_slot(p.q_off, i, p.q_tokens, p.pack, 32)) * 32, rows = (int64_t)q.len * p.pack;
+    const AttnPlace place = attn_find_slot(p.q_off, p.b, p.q_tokens, p.pack, 32, slot, p.n_slots);
+    const AttnSeq q = place.s, k = p.k_off == p.q_off ? q : attn_seq(p.k_off, place.i, p.k_tokens);
+    const int64_t first = (slot - place.first) * 32, rows = (int64_t)q.len * p.pack;
     if (first < 0 || first >= rows)
         return;
     const int64_t row = first + (lane & 31);

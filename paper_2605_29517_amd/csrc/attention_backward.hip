@@ -15,6 +15,10 @@ namespace {
 constexpr int NW = 4;
 constexpr int TILE = 64;   // keys per step of the dQ kernel
 constexpr int Q_TILE = 32; // query rows per step of the dK, dV kernel
+// Up to so many tiles of keys, delta is summed from P dP in a pass of its own instead of read off dO and O. What the rounding of O
+// puts into delta shows in dQ and dK where a row looks at few keys (1.6 to 1.9 times the rounding of the output for texts of 64 to 300 tokens), and
+// the rows that see few keys bring the largest gradients of a causal sequence too; there the pass costs little, since it needs no O.
+constexpr int EXACT_TILES = 6;
 constexpr float LOG2E = 1.44269504088896341f;
 
 template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 2) attn_dq_kernel(AttnParams p)
@@ -28,9 +32,9 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 2) attn_dq_
     const int v = xcd_grouped(blockIdx.x, gridDim.x); // (as in the forward)
     const int slot = p.n_slots - 1 - v % p.n_slots, hk = v / p.n_slots;
 
-    const int64_t i = attn_find_slot(p.q_off, p.b, p.q_tokens, p.pack, ROWS, slot);
-    const AttnSeq q = attn_seq(p.q_off, i, p.q_tokens), k = attn_seq(p.k_off, i, p.k_tokens);
-    const int64_t first = (int64_t)(slot - attn_first_slot(p.q_off, i, p.q_tokens, p.pack, ROWS)) * ROWS, rows = (int64_t)q.len * p.pack;
+    const AttnPlace place = attn_find_slot(p.q_off, p.b, p.q_tokens, p.pack, ROWS, slot, p.n_slots);
+    const AttnSeq q = place.s, k = p.k_off == p.q_off ? q : attn_seq(p.k_off, place.i, p.k_tokens);
+    const int64_t first = (slot - place.first) * ROWS, rows = (int64_t)q.len * p.pack;
     if (first < 0 || first >= rows)
         return;
 
@@ -42,7 +46,7 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 2) attn_dq_
     const int limit = p.causal ? max(0, min(k.len, token + ahead + 1)) : k.len;
     const int64_t wg_last = min(first + ROWS, rows) - 1;
     const int wg_keys = p.causal ? max(0, min(k.len, (int)(wg_last / p.pack) + ahead + 1)) : k.len;
-    const int wave_keys = __builtin_amdgcn_readlane(limit, 31), all_keys = __builtin_amdgcn_readfirstlane(limit);
+    const int wave_keys = first + w * 32 < rows ? __builtin_amdgcn_readlane(limit, 31) : 0, all_keys = __builtin_amdgcn_readfirstlane(limit);
 
     const char *k_head = p.K.p + k.start * p.K.token + hk * p.K.head, *v_head = p.V.p + k.start * p.V.token + hk * p.V.head;
     AttnCopy<DP, TILE, NW> copy;
@@ -50,23 +54,24 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 2) attn_dq_
     const AttnRowRead<DP> row_read(lane);
     const AttnColRead<DP> col_read(lane);
     const int tiles = (wg_keys + TILE - 1) / TILE;
-    auto issue = [&](int t) {
-        const uint32_t to = attn_lds(lds) + (t & 1) * 2 * TILE_BYTES;
+    const bool exact = tiles <= EXACT_TILES;
+    auto issue = [&](int buffer, int t) {
+        const uint32_t to = attn_lds(lds) + buffer * 2 * TILE_BYTES;
         copy.issue(k_head, p.K.token, t * TILE, k.len - 1, to, w);
         copy.issue(v_head, p.V.token, t * TILE, k.len - 1, to + TILE_BYTES, w);
     };
     if (tiles)
-        issue(0);
+        issue(0, 0);
 
     uint4 qf[U], gf[U];
     const int64_t at = q.start + token;
     attn_load_row(p.Q.p + at * p.Q.token + head * p.Q.head, p.d, h, qf);
     attn_load_row(p.dO.p + at * p.dO.token + head * p.dO.head, p.d, h, gf);
+    float lse2 = p.lse[at * p.hq + head] * LOG2E;
     float delta = 0.0f;
-    {
+    if (!exact) {
         uint4 of[U];
         attn_load_row(p.O.p + at * p.O.token + head * p.O.head, p.d, h, of);
-        attn_have_row(p.d, h, qf);
         attn_have_row(p.d, h, gf);
         attn_have_row(p.d, h, of);
 #pragma unroll
@@ -80,10 +85,49 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 2) attn_dq_
         }
         delta = attn_halves_sum(delta);
     }
-    float lse2 = p.lse[at * p.hq + head] * LOG2E;
+    attn_have_row(p.d, h, qf);
+    attn_have_row(p.d, h, gf);
     asm volatile("" : "+v"(lse2)); // (arrived)
-    if (row < rows)
-        p.stat[(2 * (int64_t)head + h) * p.q_tokens + at] = h ? -delta : -lse2 / p.scale_log2;
+
+    // P and dP + from of a block of 32 keys
+    auto scores = [&](const char *kt, const char *vt, int b, int key, float from, f32x16 &s, f32x16 &g) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            s[r] = 0.0f;
+            g[r] = from;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            attn_mma<DT>(row_read.get(kt, b, u), qf[u], s);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            attn_mma<DT>(row_read.get(vt, b, u), gf[u], g);
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], p.scale_log2, -lse2));
+        if (key + 32 > all_keys) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                s[r] = key + acc_row(r, h) < limit ? s[r] : 0.0f;
+        }
+    };
+    int buffer = 0;
+    if (exact) {
+        for (int t = 0; t < tiles; ++t) {
+            attn_arrive();
+            issue(buffer ^ 1, t + 1 < tiles ? t + 1 : 0);
+            const char *kt = lds + buffer * 2 * TILE_BYTES, *vt = kt + TILE_BYTES;
+            buffer ^= 1;
+            for (int b = 0; b < 2 && t * TILE + 32 * b < wave_keys; ++b) {
+                f32x16 s, g;
+                scores(kt, vt, b, t * TILE + 32 * b, 0.0f, s, g);
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    delta = __builtin_fmaf(s[r], g[r], delta);
+            }
+        }
+        delta = attn_halves_sum(delta);
+    }
 
     f32x16 dq[NB];
 #pragma unroll
@@ -91,37 +135,18 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 2) attn_dq_
 #pragma unroll
         for (int r = 0; r < 16; ++r)
             dq[b][r] = 0.0f;
-
     for (int t = 0; t < tiles; ++t) {
         attn_arrive();
         if (t + 1 < tiles)
-            issue(t + 1);
-        const char *kt = lds + (t & 1) * 2 * TILE_BYTES, *vt = kt + TILE_BYTES;
-        const int key0 = t * TILE;
-        if (key0 >= wave_keys)
-            continue;
+            issue(buffer ^ 1, t + 1);
+        const char *kt = lds + buffer * 2 * TILE_BYTES, *vt = kt + TILE_BYTES;
+        buffer ^= 1;
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
+            if (t * TILE + 32 * b >= wave_keys)
+                break;
             f32x16 s, g;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                s[r] = 0.0f;
-                g[r] = -delta; // (dP - delta: the sums start there)
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                attn_mma<DT>(row_read.get(kt, b, u), qf[u], s);
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                attn_mma<DT>(row_read.get(vt, b, u), gf[u], g);
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], p.scale_log2, -lse2));
-            if (key0 + 32 * b + 32 > all_keys) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    s[r] = key0 + 32 * b + acc_row(r, h) < limit ? s[r] : 0.0f;
-            }
+            scores(kt, vt, b, t * TILE + 32 * b, -delta, s, g); // (the sums of dP start at -delta)
 #pragma unroll
             for (int r = 0; r < 16; ++r)
                 s[r] *= g[r];
@@ -134,6 +159,8 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 2) attn_dq_
             }
         }
     }
+    if (row < rows)
+        p.stat[(2 * (int64_t)head + h) * p.q_tokens + at] = h ? -delta : -lse2 / p.scale_log2;
     if (row >= rows)
         return;
     char *to = p.dQ.p + at * p.dQ.token + head * p.dQ.head;
@@ -146,7 +173,7 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 2) attn_dq_
 }
 
 // A wavefront owns 32 keys (columns) of one key head.
-template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 2) attn_dkv_kernel(AttnParams p)
+template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, DP > 64 ? 2 : 3) attn_dkv_kernel(AttnParams p)
 {
     constexpr int KEYS = NW * 32, U = DP / 16, NB = DP / 32;
     constexpr int TILE_BYTES = Q_TILE * DP * 2, BUF = 2 * TILE_BYTES + 256; // Q, dO, 32 of -lse / scale, 32 of -delta
@@ -157,9 +184,9 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 2) attn_dkv
     const int v = xcd_grouped(blockIdx.x, gridDim.x); // (the first tiles, which the most queries see under a causal mask, come first)
     const int slot = v % p.n_slots, hk = v / p.n_slots;
 
-    const int64_t i = attn_find_slot(p.k_off, p.b, p.k_tokens, 1, KEYS, slot);
-    const AttnSeq q = attn_seq(p.q_off, i, p.q_tokens), k = attn_seq(p.k_off, i, p.k_tokens);
-    const int64_t first_ = (int64_t)(slot - attn_first_slot(p.k_off, i, p.k_tokens, 1, KEYS)) * KEYS;
+    const AttnPlace place = attn_find_slot(p.k_off, p.b, p.k_tokens, 1, KEYS, slot, p.n_slots);
+    const AttnSeq k = place.s, q = p.k_off == p.q_off ? k : attn_seq(p.q_off, place.i, p.q_tokens);
+    const int64_t first_ = (slot - place.first) * KEYS;
     if (first_ < 0 || first_ >= k.len)
         return;
     const int first = (int)first_, ahead = k.len - q.len;
@@ -212,7 +239,7 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 2) attn_dkv
         const int row0 = tile * Q_TILE;
         if (++tile == q1)
             tile = q0;
-        if (p.causal && row0 + Q_TILE - 1 + ahead < wave_key)
+        if (wave_key >= k.len || (p.causal && row0 + Q_TILE - 1 + ahead < wave_key))
             continue;
         // the sums start from what is subtracted from them: S - lse / scale, dP - delta
         f32x16 s, g;
