@@ -139,9 +139,9 @@ int attention_sizes_ok(int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, in
         return MAXSIM_ERR_INVALID;
     if (d % 8 != 0 || d > 128 || hq > (1 << 16))
         return MAXSIM_ERR_UNSUPPORTED;
-    // tiles and rows are counted in int32: (tokens / 32 + sequences) tiles of every head, tokens * heads rows of a sequence
-    const int64_t most = int64_t(1) << 31;
-    if (q_tokens >= most || k_tokens >= most || b >= most || (q_tokens / 32 + k_tokens / 32 + 2 * b) * hq >= (int64_t(1) << 25))
+    // tiles and rows are counted in 31 bits: tokens * heads rows, (rows / 32 + sequences) tiles of every head
+    const int64_t most = int64_t(1) << 30;
+    if (q_tokens >= most || k_tokens >= most || b >= (int64_t(1) << 24) || (q_tokens + 32 * b) * hq >= most || (k_tokens / 128 + b) * hkv >= most)
         return MAXSIM_ERR_UNSUPPORTED;
     return MAXSIM_OK;
 }
@@ -178,9 +178,9 @@ int attention_common(maxsim::AttnParams &p, const AttnTensor *t, int n, const in
         return MAXSIM_ERR_SCRATCH;
     p.q_off = q_offsets;
     p.k_off = k_offsets;
-    p.b = b;
-    p.q_tokens = q_tokens;
-    p.k_tokens = k_tokens;
+    p.b = (int)b;
+    p.q_tokens = (int)q_tokens;
+    p.k_tokens = (int)k_tokens;
     p.hq = hq;
     p.hkv = hkv;
     p.d = d;
@@ -612,8 +612,6 @@ int maxsim_attention_backward(const void *Q, const void *K, const void *V, const
         return rc;
     if (!lse || !aligned(lse, 4))
         return MAXSIM_ERR_INVALID;
-    if (q_tokens >= (int64_t(1) << 30)) // two rows of q_tokens floats are addressed in 32 bits
-        return MAXSIM_ERR_UNSUPPORTED;
     p.lse = const_cast<float *>(lse); // (read)
     if (int rc = ensure_init())
         return rc;

@@ -20,30 +20,50 @@ struct AttnRows { // a packed tensor [tokens, heads, d], strides in bytes
     uint32_t token; // (below 2^25: a tile's rows are addressed in 32 bits)
 };
 
+// Division of n < 2^31 by a number that the launch knows
+struct AttnDivisor {
+    uint32_t by, mul, shift;
+    static AttnDivisor of(uint32_t by)
+    {
+        uint32_t s = 0;
+        while ((uint64_t(1) << s) < by)
+            ++s;
+        return {by, (uint32_t)((uint64_t(1) << (31 + s)) / by + 1), 31 + s}; // (exact: n times the excess of mul * by is below 2^(31 + s))
+    }
+    __device__ __forceinline__ int quotient(int n) const { return (int)(((uint64_t)(uint32_t)n * mul) >> shift); }
+    __device__ __forceinline__ int operator()(int &n) const // leaves the remainder
+    {
+        const int q = quotient(n);
+        n -= q * (int)by;
+        return q;
+    }
+};
+
 struct AttnParams {
     AttnRows Q, K, V, O, dO, dQ, dK, dV;
     const int32_t *q_off, *k_off; // [b + 1]
     float *lse;                   // [q_tokens, hq]
     float *part_o, *part_lse;     // [n_split, q_tokens, hq, d], [n_split, q_tokens, hq]: partial results of the split forward
     float *stat;                  // [hq, 2, q_tokens]: -lse / scale and -delta (the backward's own)
-    int64_t b, q_tokens, k_tokens;
+    int b, q_tokens, k_tokens;
     int hq, hkv, d;
-    int pack;     // query heads that share a row block: row r of a sequence is token r / pack, head r % pack of the group
-    int n_slots;  // see attn_find_slot
-    int n_split;  // pieces of the keys
+    // query heads that share keys: row r of a sequence is token r / pack, head r % pack of the group (there are less than 2^30 rows)
+    int pack;
+    int n_slots; // see attn_find_slot
+    int n_split; // pieces of the keys
+    AttnDivisor by_pack, by_slots, by_split, by_hkv;
     int causal;
     float scale, scale_log2; // scale_log2 = scale * log2(e)
 };
 
 // Rows of one sequence
 struct AttnSeq {
-    int64_t start;
-    int len;
+    int start, len;
 };
-__device__ __forceinline__ AttnSeq attn_seq(const int32_t *off, int64_t i, int64_t tokens)
+__device__ __forceinline__ AttnSeq attn_seq(const int32_t *off, int i, int tokens)
 {
-    const int64_t s = clamp_offset(off[i], 0, tokens), e = clamp_offset(off[i + 1], s, tokens);
-    return {s, (int)(e - s)};
+    const int s = min(max(off[i], 0), tokens), e = min(max(off[i + 1], s), tokens);
+    return {s, e - s};
 }
 
 // Whether a sequence has tile t of `rows` rows is not known to the host, which has no lengths. Sequence i gets the tile slots
@@ -52,37 +72,36 @@ __device__ __forceinline__ AttnSeq attn_seq(const int32_t *off, int64_t i, int64
 // search over the offsets. Each step of a search is a round trip to memory before anything else can start: the first looks at the 64
 // sequences around the place that equal lengths would give, and mostly ends it (always up to 63 sequences). All lanes active, slot uniform.
 struct AttnPlace {
-    int64_t i, first; // the sequence, and its first slot
+    int i, first; // the sequence, and its first slot
     AttnSeq s;
 };
-__device__ __forceinline__ AttnPlace attn_find_slot(const int32_t *off, int64_t b, int64_t tokens, int mul, int rows, int slot, int n_slots)
+template <int ROWS> __device__ __forceinline__ AttnPlace attn_find_slot(const int32_t *off, int b, int tokens, int mul, int slot, int n_slots)
 {
-    const int64_t guess = (int64_t)((float)slot * (float)b / (float)n_slots) - 32;
-    const int64_t lo = guess > b - 63 ? (b > 63 ? b - 63 : 0) : guess < 0 ? 0 : guess;
-    const int64_t at = lo + (threadIdx.x & 63);
-    const int64_t v = clamp_offset(off[at < b ? at : b], 0, tokens);
-    const uint64_t below = __builtin_amdgcn_ballot_w64(at < b && v * mul / rows + at <= slot);
+    const int guess = (int)((float)slot * (float)b * __builtin_amdgcn_rcpf((float)n_slots)) - 32;
+    const int lo = __builtin_amdgcn_readfirstlane(max(min(guess, b - 63), 0));
+    const int at = lo + (threadIdx.x & 63);
+    const int v = min(max(off[min(at, b)], 0), tokens);
+    const uint64_t below = __builtin_amdgcn_ballot_w64(at < b && (int)((uint32_t)v * (uint32_t)mul / ROWS) + at <= slot);
     const int n = __builtin_popcountll(below);
     AttnPlace x;
     if (n > 0 && n < 64) {
         x.i = lo + n - 1;
-        x.s.start = (uint32_t)__builtin_amdgcn_readlane((int)v, n - 1);
-        const int64_t end = (uint32_t)__builtin_amdgcn_readlane((int)v, n);
-        x.s.len = (int)(end > x.s.start ? end - x.s.start : 0);
+        x.s.start = __builtin_amdgcn_readlane(v, n - 1);
+        x.s.len = max(__builtin_amdgcn_readlane(v, n) - x.s.start, 0);
     } else {
         OffsetSearch s; // the first i in [0, b) with first(i) > slot, b if there is none
         s.begin(b - 1);
         while (s.open()) {
             const uint32_t p = s.probe(threadIdx.x & 63);
             const bool in = p < s.end;
-            const int64_t first = clamp_offset(off[in ? p : 0u], 0, tokens) * mul / rows + p;
+            const int first = (int)((uint32_t)min(max(off[in ? p : 0u], 0), tokens) * (uint32_t)mul / ROWS) + (int)p;
             s.narrow(__builtin_amdgcn_ballot_w64(in && first <= slot));
         }
-        const uint32_t i = __builtin_amdgcn_readfirstlane(s.lo);
-        x.i = i ? (int64_t)i - 1 : 0;
+        const int i = __builtin_amdgcn_readfirstlane(s.lo);
+        x.i = max(i - 1, 0);
         x.s = attn_seq(off, x.i, tokens);
     }
-    x.first = x.s.start * mul / rows + x.i;
+    x.first = (int)((uint32_t)x.s.start * (uint32_t)mul / ROWS) + x.i;
     return x;
 }
 
@@ -134,7 +153,7 @@ template <int DP, int ROWS, int NW, bool ONCE = false> struct AttnCopy {
     // rows row0 .. of the head that starts at `head` (uniform); row0 <= last
     __device__ __forceinline__ void issue(const char *head, uint32_t token_stride, int row0, int last, uint32_t tile, int w) const
     {
-        const char *base = head + (int64_t)row0 * token_stride;
+        const char *base = head + (uint64_t)(uint32_t)row0 * token_stride;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             if (N % NW != 0 && w + NW * i >= N)

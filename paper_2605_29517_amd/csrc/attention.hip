@@ -15,30 +15,30 @@ constexpr float NO_MAXIMUM = -1.0e30f;  // of a row that has seen no key: finite
 constexpr float LAZY = 8.0f;            // the maximum may lag by this many powers of two: P <= 2^8, far from overflow in fp16
 
 // A column's result: O = o / sum and lse, or the same of a piece
-template <int DT, int NB> __device__ __forceinline__ void attn_write(const AttnParams &p, const f32x16 (&o)[NB], float top, float sum, int piece, int64_t token, int head, int h)
+template <int DT, int NB> __device__ __forceinline__ void attn_write(const AttnParams &p, const f32x16 (&o)[NB], float top, float sum, int piece, int token, int head, int h)
 {
     const bool seen = sum > 0.0f;
     const float by = seen ? 1.0f / sum : 0.0f;
     const float lse = seen ? (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f : neg_inf();
-    const int64_t at = token * p.hq + head;
+    const int at = token * p.hq + head;
     if (p.n_split > 1) {
-        float *part = p.part_o + ((int64_t)piece * p.q_tokens * p.hq + at) * p.d;
+        float *part = p.part_o + ((int64_t)piece * (p.q_tokens * p.hq) + at) * p.d;
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int r = 0; r < 16; r += 4)
-                if (32 * b + 2 * r + 4 * h < p.d)
+                if (32 * b + 2 * r < p.d)
                     *reinterpret_cast<float4 *>(part + 32 * b + 2 * r + 4 * h) = make_float4(o[b][r] * by, o[b][r + 1] * by, o[b][r + 2] * by, o[b][r + 3] * by);
         if (h == 0)
-            p.part_lse[(int64_t)piece * p.q_tokens * p.hq + at] = lse;
+            p.part_lse[(int64_t)piece * (p.q_tokens * p.hq) + at] = lse;
         return;
     }
-    char *row = p.O.p + token * p.O.token + head * p.O.head;
+    char *row = p.O.p + (uint64_t)(uint32_t)token * p.O.token + head * p.O.head;
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int r = 0; r < 16; r += 4)
-            if (32 * b + 2 * r + 4 * h < p.d)
+            if (32 * b + 2 * r < p.d)
                 attn_store4<DT>(row, 32 * b + 2 * r + 4 * h, o[b][r] * by, o[b][r + 1] * by, o[b][r + 2] * by, o[b][r + 3] * by);
     if (p.lse && h == 0)
         p.lse[at] = lse;
@@ -55,34 +55,31 @@ template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, DP 
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // Every XCD takes a contiguous range of (kv head, tile, piece): tiles that read the same keys meet in one L2. The last tiles, which see
     // the most keys under a causal mask, come first.
-    int v = xcd_grouped(blockIdx.x, gridDim.x);
-    const int piece = v % p.n_split;
-    v /= p.n_split;
-    const int slot = p.n_slots - 1 - v % p.n_slots, hk = v / p.n_slots;
+    int v = xcd_grouped(blockIdx.x, gridDim.x), u = p.by_split(v);
+    const int piece = v, hk = p.by_slots(u), slot = p.n_slots - 1 - u;
 
-    const AttnPlace place = attn_find_slot(p.q_off, p.b, p.q_tokens, p.pack, ROWS, slot, p.n_slots);
+    const AttnPlace place = attn_find_slot<ROWS>(p.q_off, p.b, p.q_tokens, p.pack, slot, p.n_slots);
     const AttnSeq q = place.s, k = p.k_off == p.q_off ? q : attn_seq(p.k_off, place.i, p.k_tokens);
-    const int64_t first = (slot - place.first) * ROWS, rows = (int64_t)q.len * p.pack;
+    const int first = (slot - place.first) * ROWS, rows = q.len * p.pack;
     if (first < 0 || first >= rows)
         return;
 
     // this lane's row: the same in both halves
-    const int64_t row = first + w * 32 + (lane & 31);
-    const int64_t row_ok = min(row, rows - 1);
-    const int token = (int)(row_ok / p.pack);
-    const int head = hk * p.pack + (int)(row_ok % p.pack);
+    const int row = first + w * 32 + (lane & 31);
+    int head = min(row, rows - 1);
+    const int token = p.by_pack(head);
+    head += hk * p.pack;
     const int ahead = k.len - q.len; // query t sees the keys up to t + ahead
     const int limit = p.causal ? max(0, min(k.len, token + ahead + 1)) : k.len;
     // keys that the rows of the workgroup and of the wavefront see, and those that all rows of the wavefront see
-    const int64_t wg_last = min(first + ROWS, rows) - 1;
-    const int wg_keys = p.causal ? max(0, min(k.len, (int)(wg_last / p.pack) + ahead + 1)) : k.len;
+    const int wg_keys = p.causal ? max(0, min(k.len, p.by_pack.quotient(min(first + ROWS, rows) - 1) + ahead + 1)) : k.len;
     const int wave_keys = first + w * 32 < rows ? __builtin_amdgcn_readlane(limit, 31) : 0, all_keys = __builtin_amdgcn_readfirstlane(limit);
 
     uint4 qf[U];
-    const char *q_row = p.Q.p + (q.start + token) * p.Q.token + head * p.Q.head;
+    const char *q_row = p.Q.p + (uint64_t)(uint32_t)(q.start + token) * p.Q.token + head * p.Q.head;
     attn_load_row(q_row, p.d, h, qf);
 
-    const char *k_head = p.K.p + k.start * p.K.token + hk * p.K.head, *v_head = p.V.p + k.start * p.V.token + hk * p.V.head;
+    const char *k_head = p.K.p + (uint64_t)(uint32_t)k.start * p.K.token + hk * p.K.head, *v_head = p.V.p + (uint64_t)(uint32_t)k.start * p.V.token + hk * p.V.head;
     AttnCopy<DP, TILE, NW> copy;
     copy.init(w, lane, p.d);
     const AttnRowRead<DP> k_read(lane);
@@ -97,7 +94,8 @@ template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, DP 
     float top = NO_MAXIMUM, sum = 0.0f;
 
     const int tiles = (wg_keys + TILE - 1) / TILE;
-    const int t0 = (int)((int64_t)tiles * piece / p.n_split), t1 = (int)((int64_t)tiles * (piece + 1) / p.n_split);
+    int over = tiles;
+    const int per = p.by_split(over), t0 = per * piece + min(piece, over), t1 = t0 + per + (piece < over);
     auto issue = [&](int t) {
         const uint32_t to = attn_lds(lds) + (t & 1) * 2 * TILE_BYTES;
         copy.issue(k_head, p.K.token, t * TILE, k.len - 1, to, w);
@@ -194,38 +192,37 @@ template <int DT, int DP> __global__ void __launch_bounds__(NF * 64, 1) attn_few
     const int lane = threadIdx.x & 63, h = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // The heads of a piece, whose rows lie side by side, run next to each other on one XCD
-    int v = xcd_grouped(blockIdx.x, gridDim.x);
-    const int hk = v % p.hkv;
-    v /= p.hkv;
-    const int piece = v % p.n_split, slot = v / p.n_split;
+    int v = xcd_grouped(blockIdx.x, gridDim.x), u = p.by_hkv(v);
+    const int hk = v, slot = p.by_split(u), piece = u;
 
-    const AttnPlace place = attn_find_slot(p.q_off, p.b, p.q_tokens, p.pack, 32, slot, p.n_slots);
+    const AttnPlace place = attn_find_slot<32>(p.q_off, p.b, p.q_tokens, p.pack, slot, p.n_slots);
     const AttnSeq q = place.s, k = p.k_off == p.q_off ? q : attn_seq(p.k_off, place.i, p.k_tokens);
-    const int64_t first = (slot - place.first) * 32, rows = (int64_t)q.len * p.pack;
+    const int first = (slot - place.first) * 32, rows = q.len * p.pack;
     if (first < 0 || first >= rows)
         return;
-    const int64_t row = first + (lane & 31);
-    const int64_t row_ok = min(row, rows - 1);
-    const int token = (int)(row_ok / p.pack);
-    const int head = hk * p.pack + (int)(row_ok % p.pack);
+    const int row = first + (lane & 31);
+    int head = min(row, rows - 1);
+    const int token = p.by_pack(head);
+    head += hk * p.pack;
     const int ahead = k.len - q.len;
     const int limit = p.causal ? max(0, min(k.len, token + ahead + 1)) : k.len;
     const int wave_keys = __builtin_amdgcn_readlane(limit, 31), all_keys = __builtin_amdgcn_readfirstlane(limit);
 
-    const char *k_head = p.K.p + k.start * p.K.token + hk * p.K.head, *v_head = p.V.p + k.start * p.V.token + hk * p.V.head;
+    const char *k_head = p.K.p + (uint64_t)(uint32_t)k.start * p.K.token + hk * p.K.head, *v_head = p.V.p + (uint64_t)(uint32_t)k.start * p.V.token + hk * p.V.head;
     AttnCopy<DP, KEYS, 1, true> copy;
     copy.init(0, lane, p.d);
     const AttnRowRead<DP> k_read(lane);
     const AttnColRead<DP> v_read(lane);
 
     const int tiles = (wave_keys + KEYS - 1) / KEYS;
-    const int t0 = (int)((int64_t)tiles * piece / p.n_split) + w, t1 = (int)((int64_t)tiles * (piece + 1) / p.n_split);
+    int over = tiles;
+    const int per = p.by_split(over), start = per * piece + min(piece, over), t0 = start + w, t1 = start + per + (piece < over);
     const int n = t0 < t1 ? (t1 - t0 + NF - 1) / NF : 0; // tiles of this wavefront: t0, t0 + NF, ...
     char *ring = lds + w * RING * 2 * TILE_BYTES;
     auto issue_k = [&](int j) { copy.issue(k_head, p.K.token, (t0 + NF * j) * KEYS, k.len - 1, attn_lds(ring) + (j % RING) * 2 * TILE_BYTES, 0); };
     auto issue_v = [&](int j) { copy.issue(v_head, p.V.token, (t0 + NF * j) * KEYS, k.len - 1, attn_lds(ring) + (j % RING) * 2 * TILE_BYTES + TILE_BYTES, 0); };
     uint4 qf[U];
-    attn_load_row(p.Q.p + (q.start + token) * p.Q.token + head * p.Q.head, p.d, h, qf);
+    attn_load_row(p.Q.p + (uint64_t)(uint32_t)(q.start + token) * p.Q.token + head * p.Q.head, p.d, h, qf);
     attn_have_row(p.d, h, qf);
     for (int j = 0; j < RING && j < n; ++j) {
         issue_k(j);
@@ -335,7 +332,7 @@ template <int DT, int DP> __global__ void __launch_bounds__(NF * 64, 1) attn_few
 constexpr int MOST_PIECES = 256;
 template <int DT, int PIECES> __global__ void __launch_bounds__(256) attn_join_kernel(AttnParams p)
 {
-    const int64_t n = p.q_tokens * p.hq;
+    const int64_t n = (int64_t)p.q_tokens * p.hq;
     const int blocks = (p.d + 31) / 32;
     const int group = threadIdx.x >> 3, g = group % PIECES;
     const int64_t unit = (int64_t)blockIdx.x * (32 / PIECES) + group / PIECES;
@@ -445,7 +442,11 @@ hipError_t attention_launch(AttnParams p, int dtype, void *workspace, int num_cu
     p.n_slots = x.n_slots;
     p.n_split = x.n_split;
     p.part_o = static_cast<float *>(workspace);
-    p.part_lse = p.part_o + (x.n_split > 1 ? x.n_split * p.q_tokens * p.hq * (int64_t)p.d : 0);
+    p.part_lse = p.part_o + (x.n_split > 1 ? (int64_t)x.n_split * p.q_tokens * p.hq * p.d : 0);
+    p.by_pack = AttnDivisor::of(x.pack);
+    p.by_slots = AttnDivisor::of(x.n_slots);
+    p.by_split = AttnDivisor::of(x.n_split);
+    p.by_hkv = AttnDivisor::of(p.hkv);
     const unsigned grid = (unsigned)(x.n_slots * p.hkv * x.n_split);
     const hipError_t e = attn_width(p.d, [&](auto dp) {
         constexpr int DP = decltype(dp)::value;
@@ -463,7 +464,7 @@ hipError_t attention_launch(AttnParams p, int dtype, void *workspace, int num_cu
     });
     if (e != hipSuccess || x.n_split == 1)
         return e;
-    const int64_t units = p.q_tokens * p.hq * ((p.d + 31) / 32);
+    const int64_t units = (int64_t)p.q_tokens * p.hq * ((p.d + 31) / 32);
     auto join = [&](auto pieces) {
         constexpr int PIECES = decltype(pieces)::value;
         const unsigned wgs = (unsigned)((units * PIECES + 31) / 32);

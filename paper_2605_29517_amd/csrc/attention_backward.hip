@@ -29,26 +29,25 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 2) attn_dq_
 
     const int lane = threadIdx.x & 63, h = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int v = xcd_grouped(blockIdx.x, gridDim.x); // (as in the forward)
-    const int slot = p.n_slots - 1 - v % p.n_slots, hk = v / p.n_slots;
+    int v = xcd_grouped(blockIdx.x, gridDim.x); // (as in the forward)
+    const int hk = p.by_slots(v), slot = p.n_slots - 1 - v;
 
-    const AttnPlace place = attn_find_slot(p.q_off, p.b, p.q_tokens, p.pack, ROWS, slot, p.n_slots);
+    const AttnPlace place = attn_find_slot<ROWS>(p.q_off, p.b, p.q_tokens, p.pack, slot, p.n_slots);
     const AttnSeq q = place.s, k = p.k_off == p.q_off ? q : attn_seq(p.k_off, place.i, p.k_tokens);
-    const int64_t first = (slot - place.first) * ROWS, rows = (int64_t)q.len * p.pack;
+    const int first = (slot - place.first) * ROWS, rows = q.len * p.pack;
     if (first < 0 || first >= rows)
         return;
 
-    const int64_t row = first + w * 32 + (lane & 31);
-    const int64_t row_ok = min(row, rows - 1);
-    const int token = (int)(row_ok / p.pack);
-    const int head = hk * p.pack + (int)(row_ok % p.pack);
+    const int row = first + w * 32 + (lane & 31);
+    int head = min(row, rows - 1);
+    const int token = p.by_pack(head);
+    head += hk * p.pack;
     const int ahead = k.len - q.len;
     const int limit = p.causal ? max(0, min(k.len, token + ahead + 1)) : k.len;
-    const int64_t wg_last = min(first + ROWS, rows) - 1;
-    const int wg_keys = p.causal ? max(0, min(k.len, (int)(wg_last / p.pack) + ahead + 1)) : k.len;
+    const int wg_keys = p.causal ? max(0, min(k.len, p.by_pack.quotient(min(first + ROWS, rows) - 1) + ahead + 1)) : k.len;
     const int wave_keys = first + w * 32 < rows ? __builtin_amdgcn_readlane(limit, 31) : 0, all_keys = __builtin_amdgcn_readfirstlane(limit);
 
-    const char *k_head = p.K.p + k.start * p.K.token + hk * p.K.head, *v_head = p.V.p + k.start * p.V.token + hk * p.V.head;
+    const char *k_head = p.K.p + (uint64_t)(uint32_t)k.start * p.K.token + hk * p.K.head, *v_head = p.V.p + (uint64_t)(uint32_t)k.start * p.V.token + hk * p.V.head;
     AttnCopy<DP, TILE, NW> copy;
     copy.init(w, lane, p.d);
     const AttnRowRead<DP> row_read(lane);
@@ -64,7 +63,7 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 2) attn_dq_
         issue(0, 0);
 
     uint4 qf[U], gf[U];
-    const int64_t at = q.start + token;
+    const uint64_t at = (uint32_t)(q.start + token);
     attn_load_row(p.Q.p + at * p.Q.token + head * p.Q.head, p.d, h, qf);
     attn_load_row(p.dO.p + at * p.dO.token + head * p.dO.head, p.d, h, gf);
     float lse2 = p.lse[at * p.hq + head] * LOG2E;
@@ -160,7 +159,7 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 2) attn_dq_
         }
     }
     if (row < rows)
-        p.stat[(2 * (int64_t)head + h) * p.q_tokens + at] = h ? -delta : -lse2 / p.scale_log2;
+        p.stat[(int64_t)(2 * head + h) * p.q_tokens + at] = h ? -delta : -lse2 / p.scale_log2;
     if (row >= rows)
         return;
     char *to = p.dQ.p + at * p.dQ.token + head * p.dQ.head;
@@ -168,7 +167,7 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 2) attn_dq_
     for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int r = 0; r < 16; r += 4)
-            if (32 * b + 2 * r + 4 * h < p.d)
+            if (32 * b + 2 * r < p.d)
                 attn_store4<DT>(to, 32 * b + 2 * r + 4 * h, dq[b][r] * p.scale, dq[b][r + 1] * p.scale, dq[b][r + 2] * p.scale, dq[b][r + 3] * p.scale);
 }
 
@@ -181,17 +180,16 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, DP > 64 ? 2
 
     const int lane = threadIdx.x & 63, h = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int v = xcd_grouped(blockIdx.x, gridDim.x); // (the first tiles, which the most queries see under a causal mask, come first)
-    const int slot = v % p.n_slots, hk = v / p.n_slots;
+    int v = xcd_grouped(blockIdx.x, gridDim.x); // (the first tiles, which the most queries see under a causal mask, come first)
+    const int hk = p.by_slots(v), slot = v;
 
-    const AttnPlace place = attn_find_slot(p.k_off, p.b, p.k_tokens, 1, KEYS, slot, p.n_slots);
+    const AttnPlace place = attn_find_slot<KEYS>(p.k_off, p.b, p.k_tokens, 1, slot, p.n_slots);
     const AttnSeq k = place.s, q = p.k_off == p.q_off ? k : attn_seq(p.q_off, place.i, p.q_tokens);
-    const int64_t first_ = (slot - place.first) * KEYS;
-    if (first_ < 0 || first_ >= k.len)
+    const int first = (slot - place.first) * KEYS, ahead = k.len - q.len;
+    if (first < 0 || first >= k.len)
         return;
-    const int first = (int)first_, ahead = k.len - q.len;
     const int wave_key = first + w * 32, key = wave_key + (lane & 31);
-    const int64_t at = k.start + min(key, k.len - 1);
+    const uint64_t at = (uint32_t)(k.start + min(key, k.len - 1));
 
     // steps: tiles of query rows that see any of the keys, for every head of the group
     const int q0 = p.causal ? max(0, first - ahead) / Q_TILE : 0, q1 = (q.len + Q_TILE - 1) / Q_TILE;
@@ -205,10 +203,10 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, DP > 64 ? 2
     auto issue = [&](int n) {
         const int head = hk * p.pack + next_g, row0 = next_t * Q_TILE;
         const uint32_t to = attn_lds(lds) + (n & 1) * BUF;
-        copy.issue(p.Q.p + q.start * p.Q.token + head * p.Q.head, p.Q.token, row0, q.len - 1, to, w);
-        copy.issue(p.dO.p + q.start * p.dO.token + head * p.dO.head, p.dO.token, row0, q.len - 1, to + TILE_BYTES, w);
+        copy.issue(p.Q.p + (uint64_t)(uint32_t)q.start * p.Q.token + head * p.Q.head, p.Q.token, row0, q.len - 1, to, w);
+        copy.issue(p.dO.p + (uint64_t)(uint32_t)q.start * p.dO.token + head * p.dO.head, p.dO.token, row0, q.len - 1, to + TILE_BYTES, w);
         if (w == 0)
-            attn_load_lds4(p.stat + 2 * (int64_t)head * p.q_tokens + q.start + row0, (uint32_t)(min(lane & 31, q.len - 1 - row0) + h * (int)p.q_tokens) * 4, to + 2 * TILE_BYTES);
+            attn_load_lds4(p.stat + 2 * (int64_t)head * p.q_tokens + q.start + row0, (uint32_t)(min(lane & 31, q.len - 1 - row0) + h * p.q_tokens) * 4, to + 2 * TILE_BYTES);
         if (++next_t == q1) {
             next_t = q0;
             ++next_g;
@@ -295,7 +293,7 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, DP > 64 ? 2
     for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int r = 0; r < 16; r += 4)
-            if (32 * b + 2 * r + 4 * h < p.d) {
+            if (32 * b + 2 * r < p.d) {
                 attn_store4<DT>(to_k, 32 * b + 2 * r + 4 * h, dk[b][r] * p.scale, dk[b][r + 1] * p.scale, dk[b][r + 2] * p.scale, dk[b][r + 3] * p.scale);
                 attn_store4<DT>(to_v, 32 * b + 2 * r + 4 * h, dv[b][r], dv[b][r + 1], dv[b][r + 2], dv[b][r + 3]);
             }
@@ -308,15 +306,18 @@ int64_t attention_backward_workspace(int64_t b, int64_t q_tokens, int64_t k_toke
 hipError_t attention_backward_launch(AttnParams p, int dtype, void *workspace, int num_cu, hipStream_t stream)
 {
     p.pack = p.hq / p.hkv;
+    p.by_pack = AttnDivisor::of(p.pack);
     p.stat = static_cast<float *>(workspace);
     return attn_width(p.d, [&](auto dp) {
         constexpr int DP = decltype(dp)::value;
-        p.n_slots = (int)(p.q_tokens * p.pack / (NW * 32) + p.b);
+        p.n_slots = p.q_tokens * p.pack / (NW * 32) + p.b;
+        p.by_slots = AttnDivisor::of(p.n_slots);
         if (dtype == MAXSIM_F16)
             attn_dq_kernel<MAXSIM_F16, DP><<<(unsigned)(p.n_slots * p.hkv), NW * 64, 0, stream>>>(p);
         else
             attn_dq_kernel<MAXSIM_BF16, DP><<<(unsigned)(p.n_slots * p.hkv), NW * 64, 0, stream>>>(p);
-        p.n_slots = (int)(p.k_tokens / (NW * 32) + p.b);
+        p.n_slots = p.k_tokens / (NW * 32) + p.b;
+        p.by_slots = AttnDivisor::of(p.n_slots);
         if (dtype == MAXSIM_F16)
             attn_dkv_kernel<MAXSIM_F16, DP><<<(unsigned)(p.n_slots * p.hkv), NW * 64, 0, stream>>>(p);
         else
