@@ -267,6 +267,27 @@ template <int DT> __device__ __forceinline__ void attn_store4(char *row, int ent
     *reinterpret_cast<uint2 *>(row + entry * 2) = make_uint2(attn_pack2<DT>(a, b), attn_pack2<DT>(c, d));
 }
 
+// A wavefront's result, 32 columns of `by` times x, as rows of 16-bit values: through 32 rows of LDS of its own, so that a store takes whole
+// rows instead of 8 bytes of 32 of them. place(r): where row r < n goes.
+template <int DT, int DP, class Place> __device__ __forceinline__ void attn_store_tile(char *lds, const f32x16 (&x)[DP / 32], float by, int lane, int d, int n, Place &&place)
+{
+    typedef AttnTile<DP> T;
+    const int c = lane & 31, h = lane >> 5;
+#pragma unroll
+    for (int b = 0; b < DP / 32; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4)
+            *reinterpret_cast<uint2 *>(lds + c * T::ROW + (((4 * b + r / 4) ^ T::swizzle(c)) << 4) + 8 * h) =
+                make_uint2(attn_pack2<DT>(x[b][r] * by, x[b][r + 1] * by), attn_pack2<DT>(x[b][r + 2] * by, x[b][r + 3] * by));
+#pragma unroll
+    for (int k = 0; k < T::CH / 2; ++k) {
+        const int row = (k * 64 + lane) / T::CH, chunk = (k * 64 + lane) % T::CH;
+        const uint4 v = *reinterpret_cast<const uint4 *>(lds + row * T::ROW + ((chunk ^ T::swizzle(row)) << 4));
+        if (row < n && chunk * 8 < d)
+            *reinterpret_cast<uint4 *>(place(row) + chunk * 16) = v;
+    }
+}
+
 // f(integral_constant DP) for the smallest compiled width that holds d
 template <class F> hipError_t attn_width(int d, F &&f)
 {

@@ -173,9 +173,20 @@ template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, DP 
     }
 
     sum = attn_halves_sum(sum);
-    if (row >= rows)
+    if (p.n_split > 1) {
+        if (row < rows)
+            attn_write<DT>(p, o, top, sum, piece, q.start + token, head, h);
         return;
-    attn_write<DT>(p, o, top, sum, piece, q.start + token, head, h);
+    }
+    __syncthreads(); // (nobody reads the tiles any more)
+    const bool seen = sum > 0.0f;
+    attn_store_tile<DT, DP>(lds + w * 32 * DP * 2, o, seen ? 1.0f / sum : 0.0f, lane, p.d, rows - first - w * 32, [&](int r) {
+        int g = first + w * 32 + r;
+        const uint32_t t = q.start + p.by_pack(g);
+        return p.O.p + (uint64_t)t * p.O.token + (hk * p.pack + g) * p.O.head;
+    });
+    if (p.lse && h == 0 && row < rows)
+        p.lse[(q.start + token) * p.hq + head] = seen ? (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f : neg_inf();
 }
 
 // The same for few rows per sequence (single tokens against kept keys): what counts is that keys and values stream at the memory's

@@ -160,15 +160,12 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 2) attn_dq_
     }
     if (row < rows)
         p.stat[(int64_t)(2 * head + h) * p.q_tokens + at] = h ? -delta : -lse2 / p.scale_log2;
-    if (row >= rows)
-        return;
-    char *to = p.dQ.p + at * p.dQ.token + head * p.dQ.head;
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; r += 4)
-            if (32 * b + 2 * r < p.d)
-                attn_store4<DT>(to, 32 * b + 2 * r + 4 * h, dq[b][r] * p.scale, dq[b][r + 1] * p.scale, dq[b][r + 2] * p.scale, dq[b][r + 3] * p.scale);
+    __syncthreads(); // (nobody reads the tiles any more)
+    attn_store_tile<DT, DP>(lds + w * 32 * DP * 2, dq, p.scale, lane, p.d, rows - first - w * 32, [&](int r) {
+        int g = first + w * 32 + r;
+        const uint32_t t = q.start + p.by_pack(g);
+        return p.dQ.p + (uint64_t)t * p.dQ.token + (hk * p.pack + g) * p.dQ.head;
+    });
 }
 
 // A wavefront owns 32 keys (columns) of one key head.
@@ -286,17 +283,11 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, DP > 64 ? 2
                 attn_mma<DT>(col_read.get(qt, nb, x), ds, dk[nb]);
         }
     }
-    if (key >= k.len)
-        return;
-    char *to_k = p.dK.p + at * p.dK.token + hk * p.dK.head, *to_v = p.dV.p + at * p.dV.token + hk * p.dV.head;
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; r += 4)
-            if (32 * b + 2 * r < p.d) {
-                attn_store4<DT>(to_k, 32 * b + 2 * r + 4 * h, dk[b][r] * p.scale, dk[b][r + 1] * p.scale, dk[b][r + 2] * p.scale, dk[b][r + 3] * p.scale);
-                attn_store4<DT>(to_v, 32 * b + 2 * r + 4 * h, dv[b][r], dv[b][r + 1], dv[b][r + 2], dv[b][r + 3]);
-            }
+    __syncthreads(); // (nobody reads the tiles any more)
+    char *rows = lds + w * 32 * DP * 2;
+    const uint32_t token = k.start + wave_key;
+    attn_store_tile<DT, DP>(rows, dk, p.scale, lane, p.d, k.len - wave_key, [&](int r) { return p.dK.p + (uint64_t)(token + r) * p.dK.token + hk * p.dK.head; });
+    attn_store_tile<DT, DP>(rows, dv, 1.0f, lane, p.d, k.len - wave_key, [&](int r) { return p.dV.p + (uint64_t)(token + r) * p.dV.token + hk * p.dV.head; });
 }
 
 } // namespace
