@@ -169,9 +169,10 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 2) attn_dq_
 }
 
 // A wavefront owns 32 keys (columns) of one key head.
-template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, DP > 64 ? 2 : 3) attn_dkv_kernel(AttnParams p)
+constexpr int NK = 4;
+template <int DT, int DP> __global__ void __launch_bounds__(NK * 64, DP > 64 ? 2 : 3) attn_dkv_kernel(AttnParams p)
 {
-    constexpr int KEYS = NW * 32, U = DP / 16, NB = DP / 32;
+    constexpr int KEYS = NK * 32, U = DP / 16, NB = DP / 32;
     constexpr int TILE_BYTES = Q_TILE * DP * 2, BUF = 2 * TILE_BYTES + 256; // Q, dO, 32 of -lse / scale, 32 of -delta
     __shared__ __attribute__((aligned(16))) char lds[2 * BUF];
 
@@ -192,18 +193,21 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, DP > 64 ? 2
     const int q0 = p.causal ? max(0, first - ahead) / Q_TILE : 0, q1 = (q.len + Q_TILE - 1) / Q_TILE;
     const int per_head = max(0, q1 - q0), steps = per_head * p.pack;
 
-    AttnCopy<DP, Q_TILE, NW> copy;
+    AttnCopy<DP, Q_TILE, NK> copy;
     copy.init(w, lane, p.d);
-    const AttnRowRead<DP> row_read(lane);
-    const AttnColRead<DP> col_read(lane);
+    AttnRowRead<DP> row_read(lane);
+    AttnColRead<DP> col_read(lane);
     int next_g = 0, next_t = q0; // of the next copy
     auto issue = [&](int n) {
         const int head = hk * p.pack + next_g, row0 = next_t * Q_TILE;
         const uint32_t to = attn_lds(lds) + (n & 1) * BUF;
         copy.issue(p.Q.p + (uint64_t)(uint32_t)q.start * p.Q.token + head * p.Q.head, p.Q.token, row0, q.len - 1, to, w);
         copy.issue(p.dO.p + (uint64_t)(uint32_t)q.start * p.dO.token + head * p.dO.head, p.dO.token, row0, q.len - 1, to + TILE_BYTES, w);
-        if (w == 0)
-            attn_load_lds4(p.stat + 2 * (int64_t)head * p.q_tokens + q.start + row0, (uint32_t)(min(lane & 31, q.len - 1 - row0) + h * p.q_tokens) * 4, to + 2 * TILE_BYTES);
+        if (w == 0) {
+            int l = lane;
+            asm volatile("" : "+v"(l)); // (worked out here: kept, the offset is spilled)
+            attn_load_lds4(p.stat + 2 * (int64_t)head * p.q_tokens + q.start + row0, (uint32_t)(min(l & 31, q.len - 1 - row0) + (l < 32 ? 0 : p.q_tokens)) * 4, to + 2 * TILE_BYTES);
+        }
         if (++next_t == q1) {
             next_t = q0;
             ++next_g;
@@ -236,6 +240,26 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, DP > 64 ? 2
             tile = q0;
         if (wave_key >= k.len || (p.causal && row0 + Q_TILE - 1 + ahead < wave_key))
             continue;
+        // 4 U products (S, dV, dP, dK) in one stream of MFMAs whose A operands are read from LDS AHEAD of them: left to itself the
+        // compiler waits for each operand before it asks for the next one, there being few registers to spare
+        constexpr int STEPS = 4 * U, AHEAD = DP > 96 ? 2 : 3;
+        static_assert(U == 2 * NB, "as many steps over the tile's rows as over its columns");
+        uint4 a[AHEAD];
+        auto read = [&](auto step) {
+            constexpr int I = decltype(step)::value, PHASE = I / U, X = I % U;
+            if constexpr (I < STEPS) {
+                if constexpr (X == 0) // (addresses are worked out where they are used: kept from one product to another they spill)
+                    asm volatile("" : "+v"(row_read.swz), "+v"(col_read.chunk));
+                if constexpr (PHASE == 0)
+                    a[I % AHEAD] = row_read.get(qt, 0, X);
+                else if constexpr (PHASE == 1)
+                    a[I % AHEAD] = col_read.get(gt, X % NB, X / NB);
+                else if constexpr (PHASE == 2)
+                    a[I % AHEAD] = row_read.get(gt, 0, X);
+                else
+                    a[I % AHEAD] = col_read.get(qt, X % NB, X / NB);
+            }
+        };
         // the sums start from what is subtracted from them: S - lse / scale, dP - delta
         f32x16 s, g;
 #pragma unroll
@@ -243,45 +267,47 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, DP > 64 ? 2
             const f32x4 l = stat[r / 2 + h];
             s[r] = l[0], s[r + 1] = l[1], s[r + 2] = l[2], s[r + 3] = l[3];
         }
+        static_for<AHEAD>(read);
+        __builtin_amdgcn_sched_barrier(0);
+        uint4 b; // of P, then of dS
+        static_for<STEPS>([&](auto step) {
+            constexpr int I = decltype(step)::value, PHASE = I / U, X = I % U;
+            if constexpr (I == U) {
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            attn_mma<DT>(row_read.get(qt, 0, u), kf[u], s);
+                for (int r = 0; r < 16; ++r)
+                    s[r] = __builtin_amdgcn_exp2f(s[r] * p.scale_log2);
+                if (row0 + Q_TILE > q.len || (p.causal && row0 + ahead < wave_key + 31)) {
+                    const int from = p.causal ? key - ahead : 0; // the first query that sees this lane's key
 #pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-            const f32x4 d = stat[8 + r / 2 + h];
-            g[r] = d[0], g[r + 1] = d[1], g[r + 2] = d[2], g[r + 3] = d[3];
-        }
+                    for (int r = 0; r < 16; ++r) {
+                        const int t = row0 + acc_row(r, h);
+                        s[r] = t >= from && t < q.len ? s[r] : 0.0f;
+                    }
+                }
+            } else if constexpr (I == 2 * U) {
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            attn_mma<DT>(row_read.get(gt, 0, u), vf[u], g);
+                for (int r = 0; r < 16; r += 4) {
+                    const f32x4 d = stat[8 + r / 2 + h];
+                    g[r] = d[0], g[r + 1] = d[1], g[r + 2] = d[2], g[r + 3] = d[3];
+                }
+            } else if constexpr (I == 3 * U) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-            s[r] = __builtin_amdgcn_exp2f(s[r] * p.scale_log2);
-        if (row0 + Q_TILE > q.len || (p.causal && row0 + ahead < wave_key + 31)) {
-            const int from = p.causal ? key - ahead : 0; // the first query that sees this lane's key
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int t = row0 + acc_row(r, h);
-                s[r] = t >= from && t < q.len ? s[r] : 0.0f;
+                for (int r = 0; r < 16; ++r)
+                    s[r] *= g[r];
             }
-        }
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            const uint4 pf = attn_operand<DT>(s, x);
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
-                attn_mma<DT>(col_read.get(gt, nb, x), pf, dv[nb]);
-        }
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-            s[r] *= g[r];
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            const uint4 ds = attn_operand<DT>(s, x);
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
-                attn_mma<DT>(col_read.get(qt, nb, x), ds, dk[nb]);
-        }
+            if constexpr (PHASE % 2 == 1 && X % NB == 0)
+                b = attn_operand<DT>(s, X / NB);
+            if constexpr (PHASE == 0)
+                attn_mma<DT>(a[I % AHEAD], kf[X], s);
+            else if constexpr (PHASE == 1)
+                attn_mma<DT>(a[I % AHEAD], b, dv[X % NB]);
+            else if constexpr (PHASE == 2)
+                attn_mma<DT>(a[I % AHEAD], vf[X], g);
+            else
+                attn_mma<DT>(a[I % AHEAD], b, dk[X % NB]);
+            read(std::integral_constant<int, I + AHEAD>{});
+            __builtin_amdgcn_sched_barrier(0);
+        });
     }
     __syncthreads(); // (nobody reads the tiles any more)
     char *rows = lds + w * 32 * DP * 2;
@@ -307,12 +333,12 @@ hipError_t attention_backward_launch(AttnParams p, int dtype, void *workspace, i
             attn_dq_kernel<MAXSIM_F16, DP><<<(unsigned)(p.n_slots * p.hkv), NW * 64, 0, stream>>>(p);
         else
             attn_dq_kernel<MAXSIM_BF16, DP><<<(unsigned)(p.n_slots * p.hkv), NW * 64, 0, stream>>>(p);
-        p.n_slots = p.k_tokens / (NW * 32) + p.b;
+        p.n_slots = p.k_tokens / (NK * 32) + p.b;
         p.by_slots = AttnDivisor::of(p.n_slots);
         if (dtype == MAXSIM_F16)
-            attn_dkv_kernel<MAXSIM_F16, DP><<<(unsigned)(p.n_slots * p.hkv), NW * 64, 0, stream>>>(p);
+            attn_dkv_kernel<MAXSIM_F16, DP><<<(unsigned)(p.n_slots * p.hkv), NK * 64, 0, stream>>>(p);
         else
-            attn_dkv_kernel<MAXSIM_BF16, DP><<<(unsigned)(p.n_slots * p.hkv), NW * 64, 0, stream>>>(p);
+            attn_dkv_kernel<MAXSIM_BF16, DP><<<(unsigned)(p.n_slots * p.hkv), NK * 64, 0, stream>>>(p);
         return hipGetLastError();
     });
 }
