@@ -232,13 +232,13 @@ template <int DT, int DP> __global__ void __launch_bounds__(NF * 64, 1) attn_few
     char *ring = lds + w * RING * 2 * TILE_BYTES;
     auto issue_k = [&](int j) { copy.issue(k_head, p.K.token, (t0 + NF * j) * KEYS, k.len - 1, attn_lds(ring) + (j % RING) * 2 * TILE_BYTES, 0); };
     auto issue_v = [&](int j) { copy.issue(v_head, p.V.token, (t0 + NF * j) * KEYS, k.len - 1, attn_lds(ring) + (j % RING) * 2 * TILE_BYTES + TILE_BYTES, 0); };
-    uint4 qf[U];
-    attn_load_row(p.Q.p + (uint64_t)(uint32_t)(q.start + token) * p.Q.token + head * p.Q.head, p.d, h, qf);
-    attn_have_row(p.d, h, qf);
     for (int j = 0; j < RING && j < n; ++j) {
         issue_k(j);
         issue_v(j);
     }
+    uint4 qf[U];
+    attn_load_row(p.Q.p + (uint64_t)(uint32_t)(q.start + token) * p.Q.token + head * p.Q.head, p.d, h, qf);
+    attn_have_row(p.d, h, qf);
 
     f32x16 o[NB];
 #pragma unroll

@@ -34,7 +34,7 @@ struct ClipTable {
 namespace {
 
 constexpr int WG = 256;
-constexpr int CHUNK = 4096;
+constexpr int CHUNK = 2048;
 constexpr int MAX_WG = 2048; // eight to a compute unit, all resident at a time
 
 template <class T> __device__ __forceinline__ double to_double(T x) { return (double)(float)x; }
@@ -117,19 +117,18 @@ __device__ __forceinline__ double wg_sum(double x) // the same in every thread
     return s;
 }
 
-// The tensor that a chunk lies in: the last one whose first chunk is not after it (tensors without entries share their first chunk with
-// the next one and are never the last)
+// The tensor that a chunk lies in: the last one whose first chunk is not after it (a tensor without entries shares its first chunk with
+// the next one and is never that). 64 probes a step, one per lane, since a step is a round trip to memory.
 template <class Tensors> __device__ __forceinline__ int find_tensor(const Tensors &t, int n, int64_t chunk)
 {
-    int lo = 0, hi = n; // the first tensor that starts after the chunk
-    while (lo < hi) {
-        const int mid = (lo + hi) / 2;
-        if (t.chunk[mid] > chunk)
-            hi = mid;
-        else
-            lo = mid + 1;
+    int lo = 0, end = n; // tensors before lo start at or before the chunk, those from end on after it
+    while (lo < end) {
+        const int step = (end - lo + 63) >> 6, at = lo + ((threadIdx.x & 63) + 1) * step - 1;
+        const uint64_t below = __builtin_amdgcn_ballot_w64(at < end && t.chunk[at < end ? at : 0] <= chunk);
+        lo += __builtin_popcountll(below) * step;
+        end = min(end, lo + step - 1);
     }
-    return lo - 1;
+    return __builtin_amdgcn_readfirstlane(lo) - 1;
 }
 
 template <class Tensors> __global__ void __launch_bounds__(WG) clip_sum_kernel(Tensors t, int n, int64_t chunks, double *part)
