@@ -44,6 +44,7 @@ struct AttnParams {
     const int32_t *q_off, *k_off; // [b + 1]
     float *lse;                   // [q_tokens, hq]
     float *part_o, *part_lse;     // [n_split, q_tokens, hq, d], [n_split, q_tokens, hq]: partial results of the split forward
+    float *part_k, *part_v;       // [n_split, k_tokens, hkv, d]: partial sums of dK (without scale) and dV
     float *stat;                  // [hq, 2, q_tokens]: -lse / scale and -delta (the backward's own)
     int b, q_tokens, k_tokens;
     int hq, hkv, d;
@@ -137,29 +138,28 @@ __device__ __forceinline__ void attn_load_lds4(const void *base, uint32_t offset
 template <int DP, int ROWS, int NW, bool ONCE = false> struct AttnCopy {
     static constexpr int CH = DP / 8, N = ROWS * CH / 64, PER = (N + NW - 1) / NW;
     static constexpr bool EVEN = NW * 64 % (16 * CH) == 0; // a lane's rows are STEP apart, its chunk is the same in all of them
-    static constexpr int STEP = NW * 64 / CH, HELD = EVEN ? 1 : PER;
-    int row[HELD]; // this lane's row, and the byte of its chunk in it, per instruction
-    uint32_t at[HELD];
+    static constexpr int STEP = NW * 64 / CH;
+    int first; // this lane's place among the chunks of the first instruction
+    uint32_t at0;
     __device__ __forceinline__ void init(int w, int lane, int d)
     {
-#pragma unroll
-        for (int i = 0; i < HELD; ++i) {
-            const int p = (w + NW * i) * 64 + lane;
-            row[i] = p / CH;
-            const int c = (p % CH) ^ AttnTile<DP>::swizzle(row[i]);
-            at[i] = min(c, d / 8 - 1) * 16;
-        }
+        first = w * 64 + lane;
+        at0 = at(first, d);
+    }
+    static __device__ __forceinline__ uint32_t at(int place, int d) // byte in its row of the chunk that belongs to a place
+    {
+        return min((place % CH) ^ AttnTile<DP>::swizzle(place / CH), d / 8 - 1) * 16;
     }
     // rows row0 .. of the head that starts at `head` (uniform); row0 <= last
-    __device__ __forceinline__ void issue(const char *head, uint32_t token_stride, int row0, int last, uint32_t tile, int w) const
+    __device__ __forceinline__ void issue(const char *head, uint32_t token_stride, int row0, int last, uint32_t tile, int w, int d) const
     {
         const char *base = head + (uint64_t)(uint32_t)row0 * token_stride;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             if (N % NW != 0 && w + NW * i >= N)
                 break;
-            const int r = EVEN ? row[0] + STEP * i : row[EVEN ? 0 : i];
-            attn_load_lds16<ONCE>(base, (uint32_t)min(r, last - row0) * token_stride + at[EVEN ? 0 : i], tile + (w + NW * i) * 1024);
+            const int place = first + NW * 64 * i, r = EVEN ? first / CH + STEP * i : place / CH;
+            attn_load_lds16<ONCE>(base, (uint32_t)min(r, last - row0) * token_stride + (EVEN ? at0 : at(place, d)), tile + (w + NW * i) * 1024);
         }
     }
 };

@@ -98,8 +98,8 @@ template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, DP 
     const int per = p.by_split(over), t0 = per * piece + min(piece, over), t1 = t0 + per + (piece < over);
     auto issue = [&](int t) {
         const uint32_t to = attn_lds(lds) + (t & 1) * 2 * TILE_BYTES;
-        copy.issue(k_head, p.K.token, t * TILE, k.len - 1, to, w);
-        copy.issue(v_head, p.V.token, t * TILE, k.len - 1, to + TILE_BYTES, w);
+        copy.issue(k_head, p.K.token, t * TILE, k.len - 1, to, w, p.d);
+        copy.issue(v_head, p.V.token, t * TILE, k.len - 1, to + TILE_BYTES, w, p.d);
     };
     // B blocks of 32 keys of a tile; key0: the first of them
     auto step = [&](const char *kt, const char *vt, int key0) {
@@ -230,8 +230,8 @@ template <int DT, int DP> __global__ void __launch_bounds__(NF * 64, 1) attn_few
     const int per = p.by_split(over), start = per * piece + min(piece, over), t0 = start + w, t1 = start + per + (piece < over);
     const int n = t0 < t1 ? (t1 - t0 + NF - 1) / NF : 0; // tiles of this wavefront: t0, t0 + NF, ...
     char *ring = lds + w * RING * 2 * TILE_BYTES;
-    auto issue_k = [&](int j) { copy.issue(k_head, p.K.token, (t0 + NF * j) * KEYS, k.len - 1, attn_lds(ring) + (j % RING) * 2 * TILE_BYTES, 0); };
-    auto issue_v = [&](int j) { copy.issue(v_head, p.V.token, (t0 + NF * j) * KEYS, k.len - 1, attn_lds(ring) + (j % RING) * 2 * TILE_BYTES + TILE_BYTES, 0); };
+    auto issue_k = [&](int j) { copy.issue(k_head, p.K.token, (t0 + NF * j) * KEYS, k.len - 1, attn_lds(ring) + (j % RING) * 2 * TILE_BYTES, 0, p.d); };
+    auto issue_v = [&](int j) { copy.issue(v_head, p.V.token, (t0 + NF * j) * KEYS, k.len - 1, attn_lds(ring) + (j % RING) * 2 * TILE_BYTES + TILE_BYTES, 0, p.d); };
     for (int j = 0; j < RING && j < n; ++j) {
         issue_k(j);
         issue_v(j);

@@ -21,7 +21,7 @@ constexpr int Q_TILE = 32; // query rows per step of the dK, dV kernel
 constexpr int EXACT_TILES = 6;
 constexpr float LOG2E = 1.44269504088896341f;
 
-template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 2) attn_dq_kernel(AttnParams p)
+template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, NW / 2) attn_dq_kernel(AttnParams p)
 {
     constexpr int ROWS = NW * 32, U = DP / 16, NB = DP / 32;
     constexpr int TILE_BYTES = TILE * DP * 2;
@@ -56,8 +56,8 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 2) attn_dq_
     const bool exact = tiles <= EXACT_TILES;
     auto issue = [&](int buffer, int t) {
         const uint32_t to = attn_lds(lds) + buffer * 2 * TILE_BYTES;
-        copy.issue(k_head, p.K.token, t * TILE, k.len - 1, to, w);
-        copy.issue(v_head, p.V.token, t * TILE, k.len - 1, to + TILE_BYTES, w);
+        copy.issue(k_head, p.K.token, t * TILE, k.len - 1, to, w, p.d);
+        copy.issue(v_head, p.V.token, t * TILE, k.len - 1, to + TILE_BYTES, w, p.d);
     };
     if (tiles)
         issue(0, 0);
@@ -178,8 +178,8 @@ template <int DT, int DP> __global__ void __launch_bounds__(NK * 64, DP > 64 ? 2
 
     const int lane = threadIdx.x & 63, h = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    int v = xcd_grouped(blockIdx.x, gridDim.x); // (the first tiles, which the most queries see under a causal mask, come first)
-    const int hk = p.by_slots(v), slot = v;
+    int v = xcd_grouped(blockIdx.x, gridDim.x), x = p.by_split(v); // (the first tiles, which the most queries see under a causal mask, come first)
+    const int piece = v, hk = p.by_slots(x), slot = x;
 
     const AttnPlace place = attn_find_slot<KEYS>(p.k_off, p.b, p.k_tokens, 1, slot, p.n_slots);
     const AttnSeq k = place.s, q = p.k_off == p.q_off ? k : attn_seq(p.q_off, place.i, p.q_tokens);
@@ -191,18 +191,20 @@ template <int DT, int DP> __global__ void __launch_bounds__(NK * 64, DP > 64 ? 2
 
     // steps: tiles of query rows that see any of the keys, for every head of the group
     const int q0 = p.causal ? max(0, first - ahead) / Q_TILE : 0, q1 = (q.len + Q_TILE - 1) / Q_TILE;
-    const int per_head = max(0, q1 - q0), steps = per_head * p.pack;
+    const int per_head = max(0, q1 - q0);
+    int over = per_head * p.pack;
+    const int per = p.by_split(over), step0 = per * piece + min(piece, over), steps = per + (piece < over); // of this piece
 
     AttnCopy<DP, Q_TILE, NK> copy;
     copy.init(w, lane, p.d);
     AttnRowRead<DP> row_read(lane);
     AttnColRead<DP> col_read(lane);
-    int next_g = 0, next_t = q0; // of the next copy
+    int next_g = per_head ? step0 / per_head : 0, next_t = q0 + step0 - next_g * per_head; // of the next copy
     auto issue = [&](int n) {
         const int head = hk * p.pack + next_g, row0 = next_t * Q_TILE;
         const uint32_t to = attn_lds(lds) + (n & 1) * BUF;
-        copy.issue(p.Q.p + (uint64_t)(uint32_t)q.start * p.Q.token + head * p.Q.head, p.Q.token, row0, q.len - 1, to, w);
-        copy.issue(p.dO.p + (uint64_t)(uint32_t)q.start * p.dO.token + head * p.dO.head, p.dO.token, row0, q.len - 1, to + TILE_BYTES, w);
+        copy.issue(p.Q.p + (uint64_t)(uint32_t)q.start * p.Q.token + head * p.Q.head, p.Q.token, row0, q.len - 1, to, w, p.d);
+        copy.issue(p.dO.p + (uint64_t)(uint32_t)q.start * p.dO.token + head * p.dO.head, p.dO.token, row0, q.len - 1, to + TILE_BYTES, w, p.d);
         if (w == 0) {
             int l = lane;
             asm volatile("" : "+v"(l)); // (worked out here: kept, the offset is spilled)
@@ -213,6 +215,7 @@ template <int DT, int DP> __global__ void __launch_bounds__(NK * 64, DP > 64 ? 2
             ++next_g;
         }
     };
+    const int next_tile = next_t;
     if (steps)
         issue(0);
 
@@ -228,7 +231,7 @@ template <int DT, int DP> __global__ void __launch_bounds__(NK * 64, DP > 64 ? 2
         for (int r = 0; r < 16; ++r)
             dk[b][r] = dv[b][r] = 0.0f;
 
-    int tile = q0;
+    int tile = next_tile;
     for (int n = 0; n < steps; ++n) {
         attn_arrive();
         if (n + 1 < steps)
@@ -309,6 +312,21 @@ template <int DT, int DP> __global__ void __launch_bounds__(NK * 64, DP > 64 ? 2
             __builtin_amdgcn_sched_barrier(0);
         });
     }
+    if (p.n_split > 1) {
+        const int64_t part = ((int64_t)piece * p.k_tokens + k.start + key) * p.hkv + hk;
+        if (key < k.len) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4)
+                    if (32 * b + 2 * r < p.d) {
+                        const int e = 32 * b + 2 * r + 4 * h;
+                        *reinterpret_cast<float4 *>(p.part_k + part * p.d + e) = make_float4(dk[b][r], dk[b][r + 1], dk[b][r + 2], dk[b][r + 3]);
+                        *reinterpret_cast<float4 *>(p.part_v + part * p.d + e) = make_float4(dv[b][r], dv[b][r + 1], dv[b][r + 2], dv[b][r + 3]);
+                    }
+        }
+        return;
+    }
     __syncthreads(); // (nobody reads the tiles any more)
     char *rows = lds + w * 32 * DP * 2;
     const uint32_t token = k.start + wave_key;
@@ -316,31 +334,94 @@ template <int DT, int DP> __global__ void __launch_bounds__(NK * 64, DP > 64 ? 2
     attn_store_tile<DT, DP>(rows, dv, 1.0f, lane, p.d, k.len - wave_key, [&](int r) { return p.dV.p + (uint64_t)(token + r) * p.dV.token + hk * p.dV.head; });
 }
 
+// Adds the pieces up, in their order; a thread per four entries of a row
+template <int DT> __global__ void __launch_bounds__(256) attn_dkv_join_kernel(AttnParams p)
+{
+    const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x, n = (int64_t)p.k_tokens * p.hkv * p.d;
+    if (x * 4 >= n)
+        return;
+    float4 k = make_float4(0.0f, 0.0f, 0.0f, 0.0f), v = k;
+#pragma unroll 4
+    for (int s = 0; s < p.n_split; ++s) {
+        const float4 a = *reinterpret_cast<const float4 *>(p.part_k + s * n + x * 4), b = *reinterpret_cast<const float4 *>(p.part_v + s * n + x * 4);
+        k = make_float4(k.x + a.x, k.y + a.y, k.z + a.z, k.w + a.w);
+        v = make_float4(v.x + b.x, v.y + b.y, v.z + b.z, v.w + b.w);
+    }
+    const int64_t row = x * 4 / p.d;
+    const int e = (int)(x * 4 % p.d), hk = (int)(row % p.hkv);
+    const int64_t token = row / p.hkv;
+    attn_store4<DT>(p.dK.p + token * p.dK.token + hk * p.dK.head, e, k.x * p.scale, k.y * p.scale, k.z * p.scale, k.w * p.scale);
+    attn_store4<DT>(p.dV.p + token * p.dV.token + hk * p.dV.head, e, v.x, v.y, v.z, v.w);
+}
+
+// Pieces of the queries of a key tile: few key heads and short batches leave most compute units idle otherwise (one sequence of 1000 keys with one head
+// is eight workgroups). An estimate in microseconds as for the forward: a step of a workgroup takes 2 at d = 128 with the chip full, its start 5.
+int dkv_pieces(int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, int hkv, int d, int num_cu)
+{
+    const double full = 2.0 * num_cu, work = (double)(k_tokens / (NK * 32) + b) * hkv, steps = std::max(1.0, (double)q_tokens / b / Q_TILE) * (hq / hkv);
+    const double step = 2.0 * (d + 64) / 192, join = (double)k_tokens * hkv * d * 16 / 4.0e6;
+    int best_n = 1;
+    double best = 0;
+    for (int n = 1; n <= 64 && n <= std::max(1.0, steps / 4) && work * n < (1 << 24); ++n) {
+        const double time = (std::max(1.0, work * n / full) + 0.6) * (steps / n * step + 5.0) + (n > 1 ? 4.0 + n * join : 0.0);
+        if (n == 1 || time < (best_n == 1 ? 0.85 : 1.0) * best) {
+            best = time;
+            best_n = n;
+        }
+    }
+    return best_n;
+}
+
 } // namespace
 
-int64_t attention_backward_workspace(int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, int hkv, int d, int num_cu) { return q_tokens * hq * 8; }
+int64_t attention_backward_workspace(int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, int hkv, int d, int num_cu)
+{
+    const int n = dkv_pieces(b, q_tokens, k_tokens, hq, hkv, d, num_cu);
+    return (q_tokens * hq * 8 + 15) / 16 * 16 + (n > 1 ? n * k_tokens * hkv * d * 8 : 0);
+}
 
 hipError_t attention_backward_launch(AttnParams p, int dtype, void *workspace, int num_cu, hipStream_t stream)
 {
     p.pack = p.hq / p.hkv;
     p.by_pack = AttnDivisor::of(p.pack);
+    p.n_split = dkv_pieces(p.b, p.q_tokens, p.k_tokens, p.hq, p.hkv, p.d, num_cu);
+    p.by_split = AttnDivisor::of(p.n_split);
     p.stat = static_cast<float *>(workspace);
-    return attn_width(p.d, [&](auto dp) {
+    p.part_k = p.stat + ((int64_t)p.q_tokens * p.hq * 2 + 3) / 4 * 4;
+    p.part_v = p.part_k + (int64_t)p.n_split * p.k_tokens * p.hkv * p.d;
+    const hipError_t e = attn_width(p.d, [&](auto dp) {
         constexpr int DP = decltype(dp)::value;
-        p.n_slots = p.q_tokens * p.pack / (NW * 32) + p.b;
-        p.by_slots = AttnDivisor::of(p.n_slots);
-        if (dtype == MAXSIM_F16)
-            attn_dq_kernel<MAXSIM_F16, DP><<<(unsigned)(p.n_slots * p.hkv), NW * 64, 0, stream>>>(p);
+        // (rows of 64 to a workgroup where those of 128 would leave compute units idle)
+        auto dq = [&](auto nw) {
+            constexpr int W = decltype(nw)::value;
+            p.n_slots = p.q_tokens * p.pack / (W * 32) + p.b;
+            p.by_slots = AttnDivisor::of(p.n_slots);
+            if (dtype == MAXSIM_F16)
+                attn_dq_kernel<MAXSIM_F16, DP, W><<<(unsigned)(p.n_slots * p.hkv), W * 64, 0, stream>>>(p);
+            else
+                attn_dq_kernel<MAXSIM_BF16, DP, W><<<(unsigned)(p.n_slots * p.hkv), W * 64, 0, stream>>>(p);
+        };
+        if ((int64_t)p.q_tokens * p.hq < 128 * (int64_t)num_cu)
+            dq(std::integral_constant<int, 2>{});
         else
-            attn_dq_kernel<MAXSIM_BF16, DP><<<(unsigned)(p.n_slots * p.hkv), NW * 64, 0, stream>>>(p);
+            dq(std::integral_constant<int, NW>{});
         p.n_slots = p.k_tokens / (NK * 32) + p.b;
         p.by_slots = AttnDivisor::of(p.n_slots);
+        const unsigned grid = (unsigned)(p.n_slots * p.hkv * p.n_split);
         if (dtype == MAXSIM_F16)
-            attn_dkv_kernel<MAXSIM_F16, DP><<<(unsigned)(p.n_slots * p.hkv), NK * 64, 0, stream>>>(p);
+            attn_dkv_kernel<MAXSIM_F16, DP><<<grid, NK * 64, 0, stream>>>(p);
         else
-            attn_dkv_kernel<MAXSIM_BF16, DP><<<(unsigned)(p.n_slots * p.hkv), NK * 64, 0, stream>>>(p);
+            attn_dkv_kernel<MAXSIM_BF16, DP><<<grid, NK * 64, 0, stream>>>(p);
         return hipGetLastError();
     });
+    if (e != hipSuccess || p.n_split == 1)
+        return e;
+    const unsigned join = (unsigned)(((int64_t)p.k_tokens * p.hkv * p.d / 4 + 255) / 256);
+    if (dtype == MAXSIM_F16)
+        attn_dkv_join_kernel<MAXSIM_F16><<<join, 256, 0, stream>>>(p);
+    else
+        attn_dkv_join_kernel<MAXSIM_BF16><<<join, 256, 0, stream>>>(p);
+    return hipGetLastError();
 }
 
 } // namespace maxsim

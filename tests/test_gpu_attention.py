@@ -79,6 +79,14 @@ def test_few_queries_many_keys(b, lq, lk, hq, hkv, d):
         compare((b, lq, lk, causal), *inputs([lq] * b, [lk - 17 * i for i in range(b)], hq, hkv, d, "bf16"), causal)
 
 
+@pytest.mark.parametrize("lens,hq,hkv,d", [([1000], 8, 1, 128), ([700, 33], 6, 2, 80), ([2000], 1, 1, 64), ([129, 0, 1500], 16, 1, 32)])
+def test_few_key_heads(lens, hq, hkv, d):
+    """Where the queries of a key tile are taken in pieces for dK and dV."""
+    for causal in (True, False):
+        compare((lens, hq, hkv, d, causal), *inputs(lens, lens, hq, hkv, d, "bf16"), causal)
+    compare("other queries", *inputs([3 * n for n in lens], lens, hq, hkv, d, "f16"), True)
+
+
 def test_scale_and_sharp_rows():
     """Another scale, and scores of some hundreds: rows that look at one token."""
     compare("scale", *inputs([100, 50], [100, 50], 2, 2, 64, "f16"), True, scale=0.3)
