@@ -21,7 +21,7 @@ constexpr int Q_TILE = 32; // query rows per step of the dK, dV kernel
 constexpr int EXACT_TILES = 6;
 constexpr float LOG2E = 1.44269504088896341f;
 
-template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, NW / 2) attn_dq_kernel(AttnParams p)
+template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 2) attn_dq_kernel(AttnParams p)
 {
     constexpr int ROWS = NW * 32, U = DP / 16, NB = DP / 32;
     constexpr int TILE_BYTES = TILE * DP * 2;
@@ -391,20 +391,12 @@ hipError_t attention_backward_launch(AttnParams p, int dtype, void *workspace, i
     p.part_v = p.part_k + (int64_t)p.n_split * p.k_tokens * p.hkv * p.d;
     const hipError_t e = attn_width(p.d, [&](auto dp) {
         constexpr int DP = decltype(dp)::value;
-        // (rows of 64 to a workgroup where those of 128 would leave compute units idle)
-        auto dq = [&](auto nw) {
-            constexpr int W = decltype(nw)::value;
-            p.n_slots = p.q_tokens * p.pack / (W * 32) + p.b;
-            p.by_slots = AttnDivisor::of(p.n_slots);
-            if (dtype == MAXSIM_F16)
-                attn_dq_kernel<MAXSIM_F16, DP, W><<<(unsigned)(p.n_slots * p.hkv), W * 64, 0, stream>>>(p);
-            else
-                attn_dq_kernel<MAXSIM_BF16, DP, W><<<(unsigned)(p.n_slots * p.hkv), W * 64, 0, stream>>>(p);
-        };
-        if ((int64_t)p.q_tokens * p.hq < 128 * (int64_t)num_cu)
-            dq(std::integral_constant<int, 2>{});
+        p.n_slots = p.q_tokens * p.pack / (NW * 32) + p.b;
+        p.by_slots = AttnDivisor::of(p.n_slots);
+        if (dtype == MAXSIM_F16)
+            attn_dq_kernel<MAXSIM_F16, DP><<<(unsigned)(p.n_slots * p.hkv), NW * 64, 0, stream>>>(p);
         else
-            dq(std::integral_constant<int, NW>{});
+            attn_dq_kernel<MAXSIM_BF16, DP><<<(unsigned)(p.n_slots * p.hkv), NW * 64, 0, stream>>>(p);
         p.n_slots = p.k_tokens / (NK * 32) + p.b;
         p.by_slots = AttnDivisor::of(p.n_slots);
         const unsigned grid = (unsigned)(p.n_slots * p.hkv * p.n_split);
