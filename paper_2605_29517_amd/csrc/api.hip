@@ -44,6 +44,7 @@ hipError_t forward_splitd_init_device();
 hipError_t forward_wide_init_device();
 hipError_t forward_i8_init_device();
 hipError_t backward_init_device();
+hipError_t attention_backward_init_device();
 } // namespace maxsim
 
 namespace {
@@ -105,7 +106,7 @@ int ensure_init()
     if (done[dev])
         return MAXSIM_OK;
     if (maxsim::forward_wide_init_device() != hipSuccess || maxsim::forward_splitd_init_device() != hipSuccess ||
-        maxsim::forward_i8_init_device() != hipSuccess || maxsim::backward_init_device() != hipSuccess)
+        maxsim::forward_i8_init_device() != hipSuccess || maxsim::backward_init_device() != hipSuccess || maxsim::attention_backward_init_device() != hipSuccess)
         return MAXSIM_ERR_LAUNCH;
     done[dev] = true;
     return MAXSIM_OK;
@@ -137,7 +138,7 @@ int attention_sizes_ok(int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, in
 {
     if (b < 1 || q_tokens < 1 || k_tokens < 1 || hq < 1 || hkv < 1 || hq % hkv != 0 || d < 1)
         return MAXSIM_ERR_INVALID;
-    if (d % 8 != 0 || d > 128 || hq > (1 << 16))
+    if (d % 8 != 0 || d > maxsim::ATTN_WIDEST || hq > (1 << 16))
         return MAXSIM_ERR_UNSUPPORTED;
     // tiles and rows are counted in 31 bits: tokens * heads rows, (rows / 32 + sequences) tiles of every head
     const int64_t most = int64_t(1) << 30;

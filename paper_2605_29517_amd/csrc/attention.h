@@ -113,7 +113,7 @@ template <int DP> struct AttnTile {
     static constexpr int CH = DP / 8, ROW = DP * 2;
     static __device__ __forceinline__ constexpr int swizzle(int r)
     {
-        return (CH == 16 ? (r & 3) << 2 : CH == 8 ? ((r >> 1) & 1) << 2 : 0) | ((r >> 2) & 3);
+        return (CH % 16 == 0 ? (r & 3) << 2 : CH == 8 ? ((r >> 1) & 1) << 2 : 0) | ((r >> 2) & 3);
     }
 };
 
@@ -297,7 +297,12 @@ template <class F> hipError_t attn_width(int d, F &&f)
         return f(std::integral_constant<int, 64>{});
     if (d <= 96)
         return f(std::integral_constant<int, 96>{});
-    return f(std::integral_constant<int, 128>{});
+    if (d <= 128)
+        return f(std::integral_constant<int, 128>{});
+    return f(std::integral_constant<int, 256>{});
 }
+constexpr int ATTN_WIDEST = 256;
+// Keys (or query rows) of a tile in LDS, so that two tiles of two tensors take 64 KB at most
+constexpr int attn_tile(int dp) { return dp > 128 ? 32 : 64; }
 
 } // namespace maxsim

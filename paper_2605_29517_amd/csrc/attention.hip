@@ -2,7 +2,7 @@
 //
 // One pass over the keys with a running maximum and sum (in 32 bits): a workgroup owns ROWS rows (a row: one token of one query
 // head; the heads that share keys lie side by side, so that a token's whole group reads K and V once), a wavefront 32 of them, and
-// walks the keys in tiles of 64 that are copied to LDS one tile ahead. P is rounded to the inputs' 16-bit type for the second
+// walks the keys in tiles of 64 (32 at d = 256) that are copied to LDS one tile ahead. P is rounded to the inputs' 16-bit type for the second
 // product (relative error 2^-9 in bf16, 2^-12 in fp16, no more than the rounding of the output; the sum that divides it
 // stays in 32 bits).
 #include "attention.h"
@@ -10,7 +10,6 @@
 namespace maxsim {
 namespace {
 
-constexpr int TILE = 64;                // keys per step
 constexpr float NO_MAXIMUM = -1.0e30f;  // of a row that has seen no key: finite, so that no difference of infinities arises
 constexpr float LAZY = 8.0f;            // the maximum may lag by this many powers of two: P <= 2^8, far from overflow in fp16
 
@@ -46,8 +45,8 @@ template <int DT, int NB> __device__ __forceinline__ void attn_write(const AttnP
 
 template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, DP > 64 ? 2 : 4) attn_fwd_kernel(AttnParams p)
 {
-    constexpr int ROWS = NW * 32, U = DP / 16, NB = DP / 32;
-    constexpr int B = DP > 64 ? 2 : 1;
+    constexpr int ROWS = NW * 32, U = DP / 16, NB = DP / 32, TILE = attn_tile(DP);
+    constexpr int B = DP == 96 || DP == 128 ? 2 : 1;
     constexpr int TILE_BYTES = TILE * DP * 2;
     __shared__ __attribute__((aligned(16))) char lds[4 * TILE_BYTES]; // two of K, two of V
 
@@ -307,24 +306,28 @@ template <int DT, int DP> __global__ void __launch_bounds__(NF * 64, 1) attn_few
     }
     sum = attn_halves_sum(sum);
 
-    // the others' results into their rings, all of whose copies have been read
-    float *mine = reinterpret_cast<float *>(ring);
+    // the others' results, when nobody reads the rings any more
+    constexpr int RESULT = (NB * 16 + 2) * 64;
+    static_assert((NF - 1) * RESULT * 4 <= (int)sizeof(lds), "fits the rings");
+    float *results = reinterpret_cast<float *>(lds);
+    __syncthreads();
     if (w > 0) {
+        float *mine = results + (w - 1) * RESULT + lane;
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r)
-                mine[(b * 16 + r) * 64 + lane] = o[b][r];
-        mine[NB * 16 * 64 + lane] = top;
-        mine[NB * 16 * 64 + 64 + lane] = sum;
+                mine[(b * 16 + r) * 64] = o[b][r];
+        mine[NB * 16 * 64] = top;
+        mine[(NB * 16 + 1) * 64] = sum;
     }
     __syncthreads();
     if (w > 0)
         return;
 #pragma unroll
     for (int x = 1; x < NF; ++x) {
-        const float *theirs = reinterpret_cast<const float *>(lds + x * RING * 2 * TILE_BYTES);
-        const float top2 = theirs[NB * 16 * 64 + lane], sum2 = theirs[NB * 16 * 64 + 64 + lane];
+        const float *theirs = results + (x - 1) * RESULT + lane;
+        const float top2 = theirs[NB * 16 * 64], sum2 = theirs[(NB * 16 + 1) * 64];
         const float to = fmaxf(top, top2), by = __builtin_amdgcn_exp2f(top - to), by2 = __builtin_amdgcn_exp2f(top2 - to);
         top = to;
         sum = sum * by + sum2 * by2;
@@ -332,7 +335,7 @@ template <int DT, int DP> __global__ void __launch_bounds__(NF * 64, 1) attn_few
         for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r)
-                o[b][r] = o[b][r] * by + theirs[(b * 16 + r) * 64 + lane] * by2;
+                o[b][r] = o[b][r] * by + theirs[(b * 16 + r) * 64] * by2;
     }
     if (row < rows)
         attn_write<DT>(p, o, top, sum, piece, q.start + token, head, h);
@@ -424,7 +427,7 @@ AttnPlan attn_plan(int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, int hk
     // Pieces of the keys: an estimate of the time, in microseconds. A step of 64 keys of a workgroup takes 1.5 (few rows: 2.2, the
     // memory's rate) while the chip is full (two workgroups to a compute unit), a workgroup's start 5; sequences differ in
     // length, which costs some of a piece at the end; joining costs a launch and a round trip of fp32 results.
-    const double full = 2.0 * num_cu, tiles = std::max(1.0, (double)k_tokens / b / TILE), work = (double)x.n_slots * hkv;
+    const double full = 2.0 * num_cu, tiles = std::max(1.0, (double)k_tokens / b / 64), work = (double)x.n_slots * hkv;
     const double step = (x.few ? 2.2 : 1.5) * d / 128, join = (double)q_tokens * hq * d * 8 / 4.0e6;
     double best = 0;
     x.n_split = 1;

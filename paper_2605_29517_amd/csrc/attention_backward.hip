@@ -13,17 +13,16 @@ namespace maxsim {
 namespace {
 
 constexpr int NW = 4;
-constexpr int TILE = 64;   // keys per step of the dQ kernel
 constexpr int Q_TILE = 32; // query rows per step of the dK, dV kernel
-// Up to so many tiles of keys, delta is summed from P dP in a pass of its own instead of read off dO and O. What the rounding of O
+// Up to so many keys, delta is summed from P dP in a pass of its own instead of read off dO and O. What the rounding of O
 // puts into delta shows in dQ and dK where a row looks at few keys (1.6 to 1.9 times the rounding of the output for texts of 64 to 300 tokens), and
 // the rows that see few keys bring the largest gradients of a causal sequence too; there the pass costs little, since it needs no O.
-constexpr int EXACT_TILES = 6;
+constexpr int EXACT_KEYS = 384;
 constexpr float LOG2E = 1.44269504088896341f;
 
-template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 2) attn_dq_kernel(AttnParams p)
+template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, DP > 128 ? 1 : 2) attn_dq_kernel(AttnParams p)
 {
-    constexpr int ROWS = NW * 32, U = DP / 16, NB = DP / 32;
+    constexpr int ROWS = NW * 32, U = DP / 16, NB = DP / 32, TILE = attn_tile(DP);
     constexpr int TILE_BYTES = TILE * DP * 2;
     __shared__ __attribute__((aligned(16))) char lds[4 * TILE_BYTES]; // two of K, two of V
 
@@ -53,7 +52,7 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 2) attn_dq_
     const AttnRowRead<DP> row_read(lane);
     const AttnColRead<DP> col_read(lane);
     const int tiles = (wg_keys + TILE - 1) / TILE;
-    const bool exact = tiles <= EXACT_TILES;
+    const bool exact = wg_keys <= EXACT_KEYS;
     auto issue = [&](int buffer, int t) {
         const uint32_t to = attn_lds(lds) + buffer * 2 * TILE_BYTES;
         copy.issue(k_head, p.K.token, t * TILE, k.len - 1, to, w, p.d);
@@ -117,7 +116,7 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 2) attn_dq_
             issue(buffer ^ 1, t + 1 < tiles ? t + 1 : 0);
             const char *kt = lds + buffer * 2 * TILE_BYTES, *vt = kt + TILE_BYTES;
             buffer ^= 1;
-            for (int b = 0; b < 2 && t * TILE + 32 * b < wave_keys; ++b) {
+            for (int b = 0; b < TILE / 32 && t * TILE + 32 * b < wave_keys; ++b) {
                 f32x16 s, g;
                 scores(kt, vt, b, t * TILE + 32 * b, 0.0f, s, g);
 #pragma unroll
@@ -141,7 +140,7 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 2) attn_dq_
         const char *kt = lds + buffer * 2 * TILE_BYTES, *vt = kt + TILE_BYTES;
         buffer ^= 1;
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < TILE / 32; ++b) {
             if (t * TILE + 32 * b >= wave_keys)
                 break;
             f32x16 s, g;
@@ -168,13 +167,16 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, 2) attn_dq_
     });
 }
 
-// A wavefront owns 32 keys (columns) of one key head.
+// A wavefront owns 32 keys (columns) of one key head; at d = 256 the registers hold the gradients of half of d, and blockIdx.y says which.
 constexpr int NK = 4;
-template <int DT, int DP> __global__ void __launch_bounds__(NK * 64, DP > 64 ? 2 : 3) attn_dkv_kernel(AttnParams p)
+constexpr int dkv_slices(int dp) { return dp > 128 ? 2 : 1; }
+constexpr int dkv_buffer(int dp) { return 2 * Q_TILE * dp * 2 + 256; } // Q, dO, 32 of -lse / scale, 32 of -delta
+template <int DT, int DP> __global__ void __launch_bounds__(NK * 64, DP > 128 ? 1 : DP > 64 ? 2 : 3) attn_dkv_kernel(AttnParams p)
 {
-    constexpr int KEYS = NK * 32, U = DP / 16, NB = DP / 32;
-    constexpr int TILE_BYTES = Q_TILE * DP * 2, BUF = 2 * TILE_BYTES + 256; // Q, dO, 32 of -lse / scale, 32 of -delta
-    __shared__ __attribute__((aligned(16))) char lds[2 * BUF];
+    constexpr int KEYS = NK * 32, U = DP / 16, SLICES = dkv_slices(DP), SLICE = DP / SLICES, NB = SLICE / 32, C = 2 * NB;
+    const int slice = SLICES > 1 ? blockIdx.y : 0;
+    constexpr int TILE_BYTES = Q_TILE * DP * 2, BUF = dkv_buffer(DP);
+    extern __shared__ __attribute__((aligned(16))) char lds[]; // two buffers
 
     const int lane = threadIdx.x & 63, h = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -243,24 +245,23 @@ template <int DT, int DP> __global__ void __launch_bounds__(NK * 64, DP > 64 ? 2
             tile = q0;
         if (wave_key >= k.len || (p.causal && row0 + Q_TILE - 1 + ahead < wave_key))
             continue;
-        // 4 U products (S, dV, dP, dK) in one stream of MFMAs whose A operands are read from LDS AHEAD of them: left to itself the
+        // The products of S, dV, dP and dK as one stream of MFMAs whose A operands are read from LDS AHEAD of them: left to itself the
         // compiler waits for each operand before it asks for the next one, there being few registers to spare
-        constexpr int STEPS = 4 * U, AHEAD = DP > 96 ? 2 : 3;
-        static_assert(U == 2 * NB, "as many steps over the tile's rows as over its columns");
+        constexpr int TO_DV = U, TO_DP = U + C, TO_DK = 2 * U + C, STEPS = 2 * U + 2 * C, AHEAD = DP == 128 ? 2 : 3;
         uint4 a[AHEAD];
         auto read = [&](auto step) {
-            constexpr int I = decltype(step)::value, PHASE = I / U, X = I % U;
+            constexpr int I = decltype(step)::value;
             if constexpr (I < STEPS) {
-                if constexpr (X == 0) // (addresses are worked out where they are used: kept from one product to another they spill)
+                if constexpr (I == 0 || I == TO_DV || I == TO_DP || I == TO_DK) // (addresses are worked out where they are used: kept from one product to another they spill)
                     asm volatile("" : "+v"(row_read.swz), "+v"(col_read.chunk));
-                if constexpr (PHASE == 0)
-                    a[I % AHEAD] = row_read.get(qt, 0, X);
-                else if constexpr (PHASE == 1)
-                    a[I % AHEAD] = col_read.get(gt, X % NB, X / NB);
-                else if constexpr (PHASE == 2)
-                    a[I % AHEAD] = row_read.get(gt, 0, X);
+                if constexpr (I < TO_DV)
+                    a[I % AHEAD] = row_read.get(qt, 0, I);
+                else if constexpr (I < TO_DP)
+                    a[I % AHEAD] = col_read.get(gt + slice * SLICE * 2, (I - TO_DV) % NB, (I - TO_DV) / NB);
+                else if constexpr (I < TO_DK)
+                    a[I % AHEAD] = row_read.get(gt, 0, I - TO_DP);
                 else
-                    a[I % AHEAD] = col_read.get(qt, X % NB, X / NB);
+                    a[I % AHEAD] = col_read.get(qt + slice * SLICE * 2, (I - TO_DK) % NB, (I - TO_DK) / NB);
             }
         };
         // the sums start from what is subtracted from them: S - lse / scale, dP - delta
@@ -274,8 +275,8 @@ template <int DT, int DP> __global__ void __launch_bounds__(NK * 64, DP > 64 ? 2
         __builtin_amdgcn_sched_barrier(0);
         uint4 b; // of P, then of dS
         static_for<STEPS>([&](auto step) {
-            constexpr int I = decltype(step)::value, PHASE = I / U, X = I % U;
-            if constexpr (I == U) {
+            constexpr int I = decltype(step)::value;
+            if constexpr (I == TO_DV) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     s[r] = __builtin_amdgcn_exp2f(s[r] * p.scale_log2);
@@ -287,31 +288,32 @@ template <int DT, int DP> __global__ void __launch_bounds__(NK * 64, DP > 64 ? 2
                         s[r] = t >= from && t < q.len ? s[r] : 0.0f;
                     }
                 }
-            } else if constexpr (I == 2 * U) {
+            } else if constexpr (I == TO_DP) {
 #pragma unroll
                 for (int r = 0; r < 16; r += 4) {
                     const f32x4 d = stat[8 + r / 2 + h];
                     g[r] = d[0], g[r + 1] = d[1], g[r + 2] = d[2], g[r + 3] = d[3];
                 }
-            } else if constexpr (I == 3 * U) {
+            } else if constexpr (I == TO_DK) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     s[r] *= g[r];
             }
-            if constexpr (PHASE % 2 == 1 && X % NB == 0)
-                b = attn_operand<DT>(s, X / NB);
-            if constexpr (PHASE == 0)
-                attn_mma<DT>(a[I % AHEAD], kf[X], s);
-            else if constexpr (PHASE == 1)
-                attn_mma<DT>(a[I % AHEAD], b, dv[X % NB]);
-            else if constexpr (PHASE == 2)
-                attn_mma<DT>(a[I % AHEAD], vf[X], g);
+            if constexpr (I == TO_DV || I == TO_DV + NB || I == TO_DK || I == TO_DK + NB)
+                b = attn_operand<DT>(s, I == TO_DV || I == TO_DK ? 0 : 1);
+            if constexpr (I < TO_DV)
+                attn_mma<DT>(a[I % AHEAD], kf[I], s);
+            else if constexpr (I < TO_DP)
+                attn_mma<DT>(a[I % AHEAD], b, dv[(I - TO_DV) % NB]);
+            else if constexpr (I < TO_DK)
+                attn_mma<DT>(a[I % AHEAD], vf[I - TO_DP], g);
             else
-                attn_mma<DT>(a[I % AHEAD], b, dk[X % NB]);
+                attn_mma<DT>(a[I % AHEAD], b, dk[(I - TO_DK) % NB]);
             read(std::integral_constant<int, I + AHEAD>{});
             __builtin_amdgcn_sched_barrier(0);
         });
     }
+    const int d0 = slice * SLICE, d = min(p.d - d0, SLICE);
     if (p.n_split > 1) {
         const int64_t part = ((int64_t)piece * p.k_tokens + k.start + key) * p.hkv + hk;
         if (key < k.len) {
@@ -319,8 +321,8 @@ template <int DT, int DP> __global__ void __launch_bounds__(NK * 64, DP > 64 ? 2
             for (int b = 0; b < NB; ++b)
 #pragma unroll
                 for (int r = 0; r < 16; r += 4)
-                    if (32 * b + 2 * r < p.d) {
-                        const int e = 32 * b + 2 * r + 4 * h;
+                    if (32 * b + 2 * r < d) {
+                        const int e = d0 + 32 * b + 2 * r + 4 * h;
                         *reinterpret_cast<float4 *>(p.part_k + part * p.d + e) = make_float4(dk[b][r], dk[b][r + 1], dk[b][r + 2], dk[b][r + 3]);
                         *reinterpret_cast<float4 *>(p.part_v + part * p.d + e) = make_float4(dv[b][r], dv[b][r + 1], dv[b][r + 2], dv[b][r + 3]);
                     }
@@ -328,10 +330,10 @@ template <int DT, int DP> __global__ void __launch_bounds__(NK * 64, DP > 64 ? 2
         return;
     }
     __syncthreads(); // (nobody reads the tiles any more)
-    char *rows = lds + w * 32 * DP * 2;
+    char *rows = lds + w * 32 * SLICE * 2;
     const uint32_t token = k.start + wave_key;
-    attn_store_tile<DT, DP>(rows, dk, p.scale, lane, p.d, k.len - wave_key, [&](int r) { return p.dK.p + (uint64_t)(token + r) * p.dK.token + hk * p.dK.head; });
-    attn_store_tile<DT, DP>(rows, dv, 1.0f, lane, p.d, k.len - wave_key, [&](int r) { return p.dV.p + (uint64_t)(token + r) * p.dV.token + hk * p.dV.head; });
+    attn_store_tile<DT, SLICE>(rows, dk, p.scale, lane, d, k.len - wave_key, [&](int r) { return p.dK.p + (uint64_t)(token + r) * p.dK.token + hk * p.dK.head + d0 * 2; });
+    attn_store_tile<DT, SLICE>(rows, dv, 1.0f, lane, d, k.len - wave_key, [&](int r) { return p.dV.p + (uint64_t)(token + r) * p.dV.token + hk * p.dV.head + d0 * 2; });
 }
 
 // Adds the pieces up, in their order; a thread per four entries of a row
@@ -374,6 +376,14 @@ int dkv_pieces(int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, int hkv, i
 
 } // namespace
 
+// dK and dV of the widest heads take 64.5 KB of LDS
+hipError_t attention_backward_init_device()
+{
+    const int bytes = 2 * dkv_buffer(ATTN_WIDEST);
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(attn_dkv_kernel<MAXSIM_F16, ATTN_WIDEST>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    return e != hipSuccess ? e : hipFuncSetAttribute(reinterpret_cast<const void *>(attn_dkv_kernel<MAXSIM_BF16, ATTN_WIDEST>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+}
+
 int64_t attention_backward_workspace(int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, int hkv, int d, int num_cu)
 {
     const int n = dkv_pieces(b, q_tokens, k_tokens, hq, hkv, d, num_cu);
@@ -399,11 +409,11 @@ hipError_t attention_backward_launch(AttnParams p, int dtype, void *workspace, i
             attn_dq_kernel<MAXSIM_BF16, DP><<<(unsigned)(p.n_slots * p.hkv), NW * 64, 0, stream>>>(p);
         p.n_slots = p.k_tokens / (NK * 32) + p.b;
         p.by_slots = AttnDivisor::of(p.n_slots);
-        const unsigned grid = (unsigned)(p.n_slots * p.hkv * p.n_split);
+        const dim3 grid((unsigned)(p.n_slots * p.hkv * p.n_split), dkv_slices(DP));
         if (dtype == MAXSIM_F16)
-            attn_dkv_kernel<MAXSIM_F16, DP><<<grid, NK * 64, 0, stream>>>(p);
+            attn_dkv_kernel<MAXSIM_F16, DP><<<grid, NK * 64, 2 * dkv_buffer(DP), stream>>>(p);
         else
-            attn_dkv_kernel<MAXSIM_BF16, DP><<<grid, NK * 64, 0, stream>>>(p);
+            attn_dkv_kernel<MAXSIM_BF16, DP><<<grid, NK * 64, 2 * dkv_buffer(DP), stream>>>(p);
         return hipGetLastError();
     });
     if (e != hipSuccess || p.n_split == 1)

@@ -62,7 +62,7 @@ def test_lengths(lengths, dtype, hq, hkv, d, causal):
     compare((lengths, dtype, hq, hkv, d, causal), *inputs(q, q if k is None else k, hq, hkv, d, dtype), causal)
 
 
-@pytest.mark.parametrize("d", [8, 16, 24, 32, 40, 48, 56, 72, 80, 88, 96, 104, 112, 120, 128])
+@pytest.mark.parametrize("d", [8, 16, 24, 32, 40, 48, 56, 72, 80, 88, 96, 104, 112, 120, 128, 136, 160, 200, 248, 256])
 def test_widths(d):
     compare(d, *inputs([70, 9, 130], [70, 200, 131], 2, 1, d, "bf16" if d % 16 else "f16"), True)
 
@@ -72,14 +72,14 @@ def test_heads(hq, hkv):
     compare((hq, hkv), *inputs([40, 1, 150], [40, 90, 150], hq, hkv, 64, "bf16"), True)
 
 
-@pytest.mark.parametrize("b,lq,lk,hq,hkv,d", [(1, 1, 20011, 4, 1, 128), (3, 1, 5000, 8, 2, 64), (2, 30, 4097, 2, 2, 96), (1, 2, 700, 1, 1, 32)])
+@pytest.mark.parametrize("b,lq,lk,hq,hkv,d", [(1, 1, 20011, 4, 1, 128), (3, 1, 5000, 8, 2, 64), (2, 30, 4097, 2, 2, 96), (1, 2, 700, 1, 1, 32), (2, 1, 3001, 8, 1, 256)])
 def test_few_queries_many_keys(b, lq, lk, hq, hkv, d):
     """Where the keys are taken in pieces."""
     for causal in (True, False):
         compare((b, lq, lk, causal), *inputs([lq] * b, [lk - 17 * i for i in range(b)], hq, hkv, d, "bf16"), causal)
 
 
-@pytest.mark.parametrize("lens,hq,hkv,d", [([1000], 8, 1, 128), ([700, 33], 6, 2, 80), ([2000], 1, 1, 64), ([129, 0, 1500], 16, 1, 32)])
+@pytest.mark.parametrize("lens,hq,hkv,d", [([1000], 8, 1, 128), ([700, 33], 6, 2, 80), ([2000], 1, 1, 64), ([129, 0, 1500], 16, 1, 32), ([700, 5], 8, 1, 256)])
 def test_few_key_heads(lens, hq, hkv, d):
     """Where the queries of a key tile are taken in pieces for dK and dV."""
     for causal in (True, False):
@@ -250,7 +250,7 @@ def test_refusals():
     with pytest.raises(M.MaxSimError, match="must be on"):
         M.maxsim_attention(Q, K, V, qo.cpu())
     with pytest.raises(M.MaxSimError, match="unsupported|built"):
-        M.maxsim_attention(*inputs([4], [4], 1, 1, 136, "f16")[:3], R.offsets([4], DEV))
+        M.maxsim_attention(*inputs([4], [4], 1, 1, 264, "f16")[:3], R.offsets([4], DEV))
     with pytest.raises(M.MaxSimError, match="invalid"):
         M.maxsim_attention(Q, K, V, qo, scale=0.0)
     with pytest.raises(M.MaxSimError, match="rows of stride 1"):
