@@ -1,6 +1,7 @@
 // C ABI of the library: argument checks, device query, kernel selection.  See include/maxsim.h.
 #include <hip/hip_runtime.h>
 
+#include <cstring>
 #include <mutex>
 
 #include "attention.h"
@@ -50,6 +51,14 @@ hipError_t attention_backward_init_device();
 namespace {
 
 bool aligned(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+// (by its bits: the library is compiled as if there were no NaNs)
+bool is_nan(float x)
+{
+    uint32_t u;
+    memcpy(&u, &x, sizeof u);
+    return (u & 0x7fffffffu) > 0x7f800000u;
+}
 
 bool dtype_ok(int dt) { return dt == MAXSIM_F32 || dt == MAXSIM_F16 || dt == MAXSIM_BF16; }
 
@@ -159,7 +168,7 @@ int attention_common(maxsim::AttnParams &p, const AttnTensor *t, int n, const in
 {
     if (int rc = attention_sizes_ok(b, q_tokens, k_tokens, hq, hkv, d))
         return rc;
-    if (!q_offsets || !k_offsets || !aligned(q_offsets, 4) || !aligned(k_offsets, 4) || !dtype_ok(dtype) || !(scale > 0.0f) || !(scale < 1e30f))
+    if (!q_offsets || !k_offsets || !aligned(q_offsets, 4) || !aligned(k_offsets, 4) || !dtype_ok(dtype) || is_nan(scale) || scale <= 0.0f || scale >= 1e30f)
         return MAXSIM_ERR_INVALID;
     if (dtype == MAXSIM_F32)
         return MAXSIM_ERR_UNSUPPORTED;
@@ -560,7 +569,7 @@ int maxsim_rope(const void *X, int64_t tokens, int heads, int d, int64_t x_token
                 const int32_t *positions, const int32_t *offsets, int64_t b, float scale, int neighbours, int inverse, void *Y, int64_t y_token_stride, int64_t y_head_stride,
                 void *stream)
 {
-    if (!X || !Y || !freqs || tokens < 1 || heads < 1 || d < 2 || rot < 2 || rot > d || rot % 2 != 0 || !dtype_ok((int)dtype) || (offsets && b < 1) || scale != scale)
+    if (!X || !Y || !freqs || tokens < 1 || heads < 1 || d < 2 || rot < 2 || rot > d || rot % 2 != 0 || !dtype_ok((int)dtype) || (offsets && b < 1) || is_nan(scale))
         return MAXSIM_ERR_INVALID;
     if (x_token_stride < 0 || x_head_stride < 0 || y_token_stride < d || y_head_stride < d) // rows of an output lie apart
         return MAXSIM_ERR_INVALID;
@@ -624,7 +633,7 @@ int64_t maxsim_clip_workspace(int n) { return n < 1 ? 0 : maxsim::clip_workspace
 int maxsim_clip_grad_norm(const void *const *grads, void *const *out, const int64_t *numel, const int32_t *dtypes, int n, float max_norm, float *norm, void *workspace,
                           int64_t workspace_bytes, void *stream)
 {
-    if (!grads || !out || !numel || !dtypes || n < 1 || !norm || !aligned(norm, 4) || !workspace || !aligned(workspace, 16) || !(max_norm >= 0.0f))
+    if (!grads || !out || !numel || !dtypes || n < 1 || !norm || !aligned(norm, 4) || !workspace || !aligned(workspace, 16) || is_nan(max_norm) || max_norm < 0.0f)
         return MAXSIM_ERR_INVALID;
     if (workspace_bytes < maxsim::clip_workspace(n))
         return MAXSIM_ERR_SCRATCH;
