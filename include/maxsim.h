@@ -296,7 +296,7 @@ int maxsim_rope(const void *X, int64_t tokens, int heads, int d, int64_t x_token
  *   workspace  maxsim_attention_workspace(...) bytes (device, 16-byte aligned); may be NULL where that is 0
  * A query that sees no key gets O = 0 and lse = -inf.  Scores, the softmax's maximum and sum and the sums over keys are
  * fp32; probabilities are rounded to the inputs' type before they multiply V.  The result is the same on every
- * run.  What a sequence's rows hold does not reach another sequence's results.
+ * run.  What a sequence's rows hold does not reach another sequence's results.  O lies apart from the inputs.
  */
 int64_t maxsim_attention_workspace(int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, int hkv, int d);
 int maxsim_attention(const void *Q, const void *K, const void *V, const int64_t *strides, const int32_t *q_offsets,
@@ -312,7 +312,8 @@ int maxsim_attention(const void *Q, const void *K, const void *V, const int64_t 
  *   strides  HOST int64 [16]: token and head stride of Q, K, V, O, dO, dQ, dK, dV, as above; NULL: all without gaps
  *   workspace  maxsim_attention_backward_workspace(...) bytes (device, 16-byte aligned)
  * Sums are fp32 in a fixed order (no atomics): the same bits on every run.  P and dS are rounded to the inputs' type
- * before they enter the last products.
+ * before they enter the last products (dS in two parts for dQ of rows that see few keys), so that fp16 gradients want the usual
+ * loss scale: what is below 6e-8 in dS is lost.  The gradients lie apart from the inputs and from each other.
  */
 int64_t maxsim_attention_backward_workspace(int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, int hkv, int d);
 int maxsim_attention_backward(const void *Q, const void *K, const void *V, const void *O, const float *lse,

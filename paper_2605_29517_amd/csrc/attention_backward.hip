@@ -14,10 +14,13 @@ namespace {
 
 constexpr int NW = 4;
 constexpr int Q_TILE = 32; // query rows per step of the dK, dV kernel
-// Up to so many keys, delta is summed from P dP in a pass of its own instead of read off dO and O. What the rounding of O
-// puts into delta shows in dQ and dK where a row looks at few keys (1.6 to 1.9 times the rounding of the output for texts of 64 to 300 tokens), and
-// the rows that see few keys bring the largest gradients of a causal sequence too; there the pass costs little, since it needs no O.
-constexpr int EXACT_KEYS = 384;
+// What the rounding of O puts into delta = sum_d dO O shows in dQ and dK where rows look at few keys: their errors are up to 1.9 times
+// what the rounding of the outputs alone makes, where 1.41 follows from the rounding of dS. Three things keep them at 1.1 to 1.45:
+//   dK    takes delta plus the sum of dS over the row's keys, which is what delta was short of (it is zero for the right one);
+//   dQ    of rows of up to EXACT_KEYS keys: delta is summed from P dP in a pass of its own, which needs no O;
+//   dQ    of more keys: dS is rounded in two parts, so that delta's part is nearly all that is left; one product more, beside the same operand.
+// Under a causal mask rows of more than SPLIT_KEYS_CAUSAL keys bring little of the gradient, and stay as they are.
+constexpr int EXACT_KEYS = 128, SPLIT_KEYS_CAUSAL = 512;
 constexpr float LOG2E = 1.44269504088896341f;
 
 template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, DP > 128 ? 1 : 2) attn_dq_kernel(AttnParams p)
@@ -52,7 +55,7 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, DP > 128 ? 
     const AttnRowRead<DP> row_read(lane);
     const AttnColRead<DP> col_read(lane);
     const int tiles = (wg_keys + TILE - 1) / TILE;
-    const bool exact = wg_keys <= EXACT_KEYS;
+    const bool exact = wg_keys <= EXACT_KEYS, twice = !exact && (!p.causal || wg_keys <= SPLIT_KEYS_CAUSAL);
     auto issue = [&](int buffer, int t) {
         const uint32_t to = attn_lds(lds) + buffer * 2 * TILE_BYTES;
         copy.issue(k_head, p.K.token, t * TILE, k.len - 1, to, w, p.d);
@@ -133,30 +136,54 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, DP > 128 ? 
 #pragma unroll
         for (int r = 0; r < 16; ++r)
             dq[b][r] = 0.0f;
-    for (int t = 0; t < tiles; ++t) {
-        attn_arrive();
-        if (t + 1 < tiles)
-            issue(buffer ^ 1, t + 1);
-        const char *kt = lds + buffer * 2 * TILE_BYTES, *vt = kt + TILE_BYTES;
-        buffer ^= 1;
+    float rest = 0.0f; // sum of dS over the row's keys: what delta is short of
+    auto walk = [&](auto twice_) {
+        for (int t = 0; t < tiles; ++t) {
+            attn_arrive();
+            if (t + 1 < tiles)
+                issue(buffer ^ 1, t + 1);
+            const char *kt = lds + buffer * 2 * TILE_BYTES, *vt = kt + TILE_BYTES;
+            buffer ^= 1;
 #pragma unroll
-        for (int b = 0; b < TILE / 32; ++b) {
-            if (t * TILE + 32 * b >= wave_keys)
-                break;
-            f32x16 s, g;
-            scores(kt, vt, b, t * TILE + 32 * b, -delta, s, g); // (the sums of dP start at -delta)
+            for (int b = 0; b < TILE / 32; ++b) {
+                if (t * TILE + 32 * b >= wave_keys)
+                    break;
+                f32x16 s, g;
+                scores(kt, vt, b, t * TILE + 32 * b, -delta, s, g); // (the sums of dP start at -delta)
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                s[r] *= g[r];
+                for (int r = 0; r < 16; ++r) {
+                    s[r] *= g[r];
+                    rest += s[r];
+                }
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const uint4 ds = attn_operand<DT>(s, x);
+                for (int x = 0; x < 2; ++x) {
+                    const uint4 ds = attn_operand<DT>(s, x);
+                    uint4 more;
+                    if constexpr (decltype(twice_)::value) {
+                        const uint32_t u[4] = {ds.x, ds.y, ds.z, ds.w};
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb)
-                    attn_mma<DT>(col_read.get(kt, nb, 2 * b + x), ds, dq[nb]);
+                        for (int e = 0; e < 4; ++e) {
+                            s[8 * x + 2 * e] -= attn_float<DT>(u[e] & 0xffff);
+                            s[8 * x + 2 * e + 1] -= attn_float<DT>(u[e] >> 16);
+                        }
+                        more = attn_operand<DT>(s, x);
+                    }
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) {
+                        const uint4 a = col_read.get(kt, nb, 2 * b + x);
+                        attn_mma<DT>(a, ds, dq[nb]);
+                        if constexpr (decltype(twice_)::value)
+                            attn_mma<DT>(a, more, dq[nb]);
+                    }
+                }
             }
         }
-    }
+    };
+    if (twice)
+        walk(std::true_type{});
+    else
+        walk(std::false_type{});
+    delta += attn_halves_sum(rest);
     if (row < rows)
         p.stat[(int64_t)(2 * head + h) * p.q_tokens + at] = h ? -delta : -lse2 / p.scale_log2;
     __syncthreads(); // (nobody reads the tiles any more)

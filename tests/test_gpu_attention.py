@@ -87,6 +87,28 @@ def test_few_key_heads(lens, hq, hkv, d):
     compare("other queries", *inputs([3 * n for n in lens], lens, hq, hkv, d, "f16"), True)
 
 
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("n,d,dtype", [(40, 64, "bf16"), (128, 64, "f16"), (200, 128, "bf16"), (700, 64, "bf16"), (1500, 128, "f16")])
+def test_errors_in_the_norm(n, d, dtype, causal):
+    """Where every result is rounded once and one operand of its sum once (P for O and dV, dS for dK and dQ), both by u at random, the error is
+    sqrt(2) of what the rounding of the results alone makes; half as much again of that second rounding is left for delta: 1.5."""
+    Q, K, V, dO, qo, ko = inputs([n] * (1 + 300 // n), [n] * (1 + 300 // n), 8, 2, d, dtype)
+    got = run(Q, K, V, dO, qo, ko, causal)
+    want = R.attention(Q, K, V, qo, ko, causal, d ** -0.5, dO)
+    for name in ("O", "dQ", "dK", "dV"):
+        value = want[name][0]
+        alone = (value.to(Q.dtype).double() - value).norm()
+        off = (got[name].double() - value).norm()
+        print(n, d, dtype, causal, name, "%.3f" % float(off / alone), flush=True)
+        assert off <= 1.5 * alone, name
+
+
+def test_small_gradients():
+    """fp16 gradients of 10^-3: P and dS leave the range of normal numbers, which the bounds count."""
+    Q, K, V, dO, qo, ko = inputs([300, 20], [300, 20], 4, 2, 64, "f16")
+    compare("small", Q, K, V, dO * 2.0 ** -10, qo, ko, True)
+
+
 def test_scale_and_sharp_rows():
     """Another scale, and scores of some hundreds: rows that look at one token."""
     compare("scale", *inputs([100, 50], [100, 50], 2, 2, 64, "f16"), True, scale=0.3)
