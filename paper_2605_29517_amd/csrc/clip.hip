@@ -35,7 +35,7 @@ namespace {
 
 constexpr int WG = 256;
 constexpr int CHUNK = 2048;
-constexpr int MAX_WG = 2048; // eight to a compute unit, all resident at a time
+constexpr int MAX_WG = 1536; // six to a compute unit, all resident at a time (5.2 GB: 2850 us; eight 2900, four 3120; 22 MB take 18.6 with four to eight)
 // Gradients of so many bytes do not stay in the caches (256 MB before the memory) until the second pass: they are moved past them.
 // 24 layers of 2048 in fp32 (5.2 GB): 3030 us without the hint, 2900 with it; 6 layers of 384 (22 MB): 18.6 and 21.4.
 constexpr int64_t STREAM_BYTES = int64_t(256) << 20;
