@@ -7,6 +7,8 @@
 // stays in 32 bits).
 #include "attention.h"
 
+#include <cmath>
+
 namespace maxsim {
 namespace {
 
@@ -201,8 +203,8 @@ template <int DT, int DP> __global__ void __launch_bounds__(NF * 64, 1) attn_few
 
     const int lane = threadIdx.x & 63, h = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    // The heads of a piece, whose rows lie side by side, run next to each other on one XCD
-    int v = xcd_grouped(blockIdx.x, gridDim.x), u = p.by_hkv(v);
+    // (the heads of a piece, whose rows lie side by side, run at the same time)
+    int v = blockIdx.x, u = p.by_hkv(v);
     const int hk = v, slot = p.by_split(u), piece = u;
 
     const AttnPlace place = attn_find_slot<32>(p.q_off, p.b, p.q_tokens, p.pack, slot, p.n_slots);
@@ -341,11 +343,12 @@ template <int DT, int DP> __global__ void __launch_bounds__(NF * 64, 1) attn_few
         attn_write<DT>(p, o, top, sum, piece, q.start + token, head, h);
 }
 
-// Joins the pieces of a row: weights exp(lse_piece - lse). Eight lanes read 128 bytes of a piece; PIECES such groups take pieces of the
-// same row in turn (many pieces of few rows spread over the chip that way), the others of a workgroup take other rows.
+// Joins the pieces of a row: weights exp(lse_piece - lse). Eight lanes read 128 bytes of a piece; PIECES such groups, 1 or the 8 of a wavefront,
+// take pieces of the same row in turn (many pieces of few rows spread over the chip that way).
 constexpr int MOST_PIECES = 256;
 template <int DT, int PIECES> __global__ void __launch_bounds__(256) attn_join_kernel(AttnParams p)
 {
+    static_assert(PIECES == 1 || PIECES == 8, "a lane's group or its wavefront");
     const int64_t n = (int64_t)p.q_tokens * p.hq;
     const int blocks = (p.d + 31) / 32;
     const int group = threadIdx.x >> 3, g = group % PIECES;
@@ -356,52 +359,35 @@ template <int DT, int PIECES> __global__ void __launch_bounds__(256) attn_join_k
     const float *lse = p.part_lse + at;
 
     float top = NO_MAXIMUM, sum = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    auto add = [&](float by, int s) {
+    if constexpr (PIECES == 1) {
+        for (int s = 0; s < p.n_split; ++s)
+            top = fmaxf(top, lse[s * n]);
+    } else {
+        for (int s = threadIdx.x & 63; s < p.n_split; s += 64)
+            top = fmaxf(top, lse[s * n]);
+#pragma unroll
+        for (int m = 32; m; m >>= 1)
+            top = fmaxf(top, __shfl_xor(top, m, 64));
+    }
+#pragma unroll 4
+    for (int s = g; s < p.n_split; s += PIECES) {
+        const float by = __builtin_amdgcn_exp2f((lse[s * n] - top) * 1.44269504088896341f);
         const float4 y = *reinterpret_cast<const float4 *>(p.part_o + (s * n + at) * p.d + e);
         sum += by;
         o[0] = __builtin_fmaf(by, y.x, o[0]);
         o[1] = __builtin_fmaf(by, y.y, o[1]);
         o[2] = __builtin_fmaf(by, y.z, o[2]);
         o[3] = __builtin_fmaf(by, y.w, o[3]);
-    };
-    if constexpr (PIECES == 1) {
-        for (int s = 0; s < p.n_split; ++s)
-            top = fmaxf(top, lse[s * n]);
-        for (int s = 0; s < p.n_split; ++s)
-            add(__builtin_amdgcn_exp2f((lse[s * n] - top) * 1.44269504088896341f), s);
-    } else {
-        __shared__ float weight[MOST_PIECES], tops[4];
-        __shared__ float4 part[PIECES][8];
-        __shared__ float part_sum[PIECES];
-        const float mine = (int)threadIdx.x < p.n_split ? lse[threadIdx.x * n] : neg_inf();
-        top = fmaxf(top, mine);
-#pragma unroll
-        for (int m = 32; m; m >>= 1)
-            top = fmaxf(top, __shfl_xor(top, m, 64));
-        if ((threadIdx.x & 63) == 0)
-            tops[threadIdx.x >> 6] = top;
-        __syncthreads();
-        top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-        weight[threadIdx.x] = __builtin_amdgcn_exp2f((mine - top) * 1.44269504088896341f);
-        __syncthreads();
-#pragma unroll 8
-        for (int s = g; s < p.n_split; s += PIECES)
-            add(weight[s], s);
-        part[group][threadIdx.x & 7] = make_float4(o[0], o[1], o[2], o[3]);
-        part_sum[group] = sum;
-        __syncthreads();
-        if (g != 0)
-            return;
-#pragma unroll
-        for (int x = 1; x < PIECES; ++x) {
-            const float4 y = part[x][threadIdx.x & 7];
-            o[0] += y.x;
-            o[1] += y.y;
-            o[2] += y.z;
-            o[3] += y.w;
-            sum += part_sum[x];
-        }
     }
+#pragma unroll
+    for (int m = 8; m < 8 * PIECES; m <<= 1) {
+        sum += __shfl_xor(sum, m, 64);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            o[i] += __shfl_xor(o[i], m, 64);
+    }
+    if (g != 0)
+        return;
     if (!in)
         return;
     const float by = sum > 0.0f ? 1.0f / sum : 0.0f;
@@ -418,22 +404,36 @@ struct AttnPlan {
 };
 constexpr int NW = 4;
 
+// Few rows per sequence and more keys and values than FEW_BYTES: attn_few_kernel. Both kernels with their best pieces, caches cold: 64 x 8192
+// keys of two heads of 128 (537 MB) 98 us -> 92, ragged caches of 16 x 500 .. 16000 keys of eight heads (455 MB) 93 -> 87, of 32 x 100 .. 8000
+// keys of 16 heads (1.1 GB) 194 -> 182; below, its longer start counts: one sequence of 2000 keys (2 MB) 12.1 -> 13.7, 4000 of eight heads
+// (16 MB) 13.3 -> 13.8, 16 x 4000 of four heads of 64 (66 MB) 20.0 -> 21.1.
+constexpr double FEW_BYTES = 1e8;
+
 AttnPlan attn_plan(int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, int hkv, int d, int num_cu)
 {
     AttnPlan x;
     x.pack = hq / hkv;
-    x.few = q_tokens * x.pack <= 32 * b && k_tokens >= 256 * b;
-    x.n_slots = (int)(q_tokens * x.pack / (x.few ? 32 : NW * 32) + b);
-    // Pieces of the keys: an estimate of the time, in microseconds. A step of 64 keys of a workgroup takes 1.5 (few rows: 2.2, the
-    // memory's rate) while the chip is full (two workgroups to a compute unit), a workgroup's start 5; sequences differ in
-    // length, which costs some of a piece at the end; joining costs a launch and a round trip of fp32 results.
-    const double full = 2.0 * num_cu, tiles = std::max(1.0, (double)k_tokens / b / 64), work = (double)x.n_slots * hkv;
-    const double step = (x.few ? 2.2 : 1.5) * d / 128, join = (double)q_tokens * hq * d * 8 / 4.0e6;
+    const double bytes = (double)k_tokens * hkv * d * 4;
+    x.few = q_tokens * x.pack <= 32 * b && bytes >= FEW_BYTES;
+    const int rows = x.few ? 32 : NW * 32;
+    x.n_slots = (int)(q_tokens * x.pack / rows + b);
+    // Pieces of the keys: the number whose estimate is least, in microseconds. A workgroup's start takes 3, a tile of 64 keys of d = 128 1.06
+    // if it has the compute unit for itself and 1.5 beside another one; the memory gives 6.4 TB/s, and pieces of unequal sequences end at
+    // different times; joining takes a launch and a round trip of fp32 results. Over 28 shapes of one to 500 new tokens, 1 to 200
+    // sequences and 500 to 131072 keys, equal and ragged, the choice takes 3 % longer than the best number on average and 19 % at most: one
+    // token after 2000 keys of two heads 37 us in one piece, 11.7 in 12; 100 tokens after 8192 keys 141 and 27 (23 in 16 pieces).
+    const double full = 2.0 * num_cu, wgs = (double)((q_tokens * x.pack + b * rows - 1) / (b * rows)) * b * hkv, tiles = std::max(1.0, (double)k_tokens / b / 64);
+    const double width = (d + 32) / 160.0, join = (double)q_tokens * hq * d * 8 / 6.0e6;
     double best = 0;
     x.n_split = 1;
-    for (int n = 1; n <= MOST_PIECES && n <= std::max(1.0, tiles / 4) && work * n < (1 << 24); n = n < 8 ? n + 1 : n + n / 4) {
-        const double time = (std::max(1.0, work * n / full) + 0.6) * (tiles / n * step + 5.0) + (n > 1 ? 4.0 + n * join : 0.0);
-        if (n == 1 || time < (x.n_split == 1 ? 0.85 : 1.0) * best) { // (one piece unless it costs clearly more)
+    const int fill = (int)(full / wgs); // the most pieces that run at the same time
+    for (int n = 1, next; n <= MOST_PIECES && n <= std::max(1.0, tiles / 2) && (double)x.n_slots * hkv * n < (1 << 24); n = n < fill && fill < next ? fill : next) {
+        next = n < 8 ? n + 1 : n + n / 4;
+        const double rounds = std::max(1.0, wgs * n / full) + 0.2, step = 1.06 + 0.88 * std::max(0.0, std::min(1.0, wgs * n / full) - 0.5);
+        const double compute = rounds * std::ceil(tiles / n) * step * width, memory = bytes / 6.4e6 * (1 + 0.2 / n);
+        const double time = std::sqrt(compute * compute + memory * memory) + 3.0 * rounds + (n > 1 ? 3.0 + n * join : 0.0);
+        if (n == 1 || time < best) {
             best = time;
             x.n_split = n;
         }
@@ -487,10 +487,12 @@ hipError_t attention_launch(AttnParams p, int dtype, void *workspace, int num_cu
         else
             attn_join_kernel<MAXSIM_BF16, PIECES><<<wgs, 256, 0, stream>>>(p);
     };
-    if (x.n_split <= 16)
+    // 16 pieces of 256 rows of 128 (1024 units) 19.0 us with a group for a row's pieces, 13.6 with eight; of 4800 rows (19200) 46.8 and 46.5,
+    // 6 pieces of those 39.1 and 42.3, 6 of 100 rows 35.5 and 35.7
+    if (x.n_split < (units > 8192 ? 16 : 6))
         join(std::integral_constant<int, 1>{});
     else
-        join(std::integral_constant<int, 32>{});
+        join(std::integral_constant<int, 8>{});
     return hipGetLastError();
 }
 
