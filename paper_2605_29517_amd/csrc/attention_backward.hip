@@ -5,8 +5,11 @@
 //   dQ      a workgroup owns query rows and walks the keys, as the forward does: S, dP = dO V^T, dS = P (dP - delta), dQ += dS K.
 //           It also leaves what the second kernel's sums start from, -lse / scale and -delta = -sum_d dO O.
 //   dK, dV  a workgroup owns keys and walks the queries of all heads that share them: S, dP, dV += P^T dO, dK += dS^T Q.
-// Scores and dP are thus computed twice, seven products instead of five; adding dQ up from the second kernel would need an
-// fp32 array of dQ and atomics. P and dS are rounded to the inputs' type for the last products (as P is in the forward).
+// Scores and dP are thus computed twice, seven products instead of five (eight where dS is kept in two parts, nine in the exact pass); adding dQ
+// up from the second kernel would need an fp32 array of dQ and atomics. P and dS are rounded to the inputs' type for the last products (as P is
+// in the forward). Bound, as the forward, by the matrix units under the power limit where sequences are long: 4 x 4096 causal tokens of 32
+// heads of 128 over 8 take 750 us (dQ) and 1090-1200 (dK, dV; 57-64 % of the units' time at 1.8 GHz); 250 texts of 64 to 300 tokens, 12 heads of 64,
+// 115 and 118 us, bound by latency.
 #include "attention.h"
 
 namespace maxsim {
@@ -19,7 +22,8 @@ constexpr int Q_TILE = 32; // query rows per step of the dK, dV kernel
 //   dK    takes delta plus the sum of dS over the row's keys, which is what delta was short of (it is zero for the right one);
 //   dQ    of rows of up to EXACT_KEYS keys: delta is summed from P dP in a pass of its own, which needs no O;
 //   dQ    of more keys: dS is rounded in two parts, so that delta's part is nearly all that is left; one product more, beside the same operand.
-// Under a causal mask rows of more than SPLIT_KEYS_CAUSAL keys bring little of the gradient, and stay as they are.
+// Under a causal mask rows of more than SPLIT_KEYS_CAUSAL keys bring little of the gradient, and stay as they are. What the last two cost: 500 texts
+// of 100 tokens, 16 heads of 128 over 4, 379 us of gradient without, 396 with; 64 x 1024 tokens of 12 heads of 64, no mask, 745 and 826.
 constexpr int EXACT_KEYS = 128, SPLIT_KEYS_CAUSAL = 512;
 constexpr float LOG2E = 1.44269504088896341f;
 
@@ -194,6 +198,8 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, DP > 128 ? 
     });
 }
 
+// NK: wavefronts of 32 keys, which share the tiles of queries; the gradient of 4 x 4096 causal tokens, 32 heads of 128 over 8, took 2626 us with one, 2091 with two, 1997
+// with four and 2037 with eight.
 // A wavefront owns 32 keys (columns) of one key head; at d = 256 the registers hold the gradients of half of d, and blockIdx.y says which.
 constexpr int NK = 4;
 constexpr int dkv_slices(int dp) { return dp > 128 ? 2 : 1; }
@@ -273,7 +279,8 @@ template <int DT, int DP> __global__ void __launch_bounds__(NK * 64, DP > 128 ? 
         if (wave_key >= k.len || (p.causal && row0 + Q_TILE - 1 + ahead < wave_key))
             continue;
         // The products of S, dV, dP and dK as one stream of MFMAs whose A operands are read from LDS AHEAD of them: left to itself the
-        // compiler waits for each operand before it asks for the next one, there being few registers to spare
+        // compiler waits for each operand before it asks for the next one, there being few registers to spare. (Three ahead spill at d = 128:
+        // 16 x 1024 causal tokens of 16 heads over 4, dQ, dK and dV 341 us, two 314; at d = 256 three 886, two 894.)
         constexpr int TO_DV = U, TO_DP = U + C, TO_DK = 2 * U + C, STEPS = 2 * U + 2 * C, AHEAD = DP == 128 ? 2 : 3;
         uint4 a[AHEAD];
         auto read = [&](auto step) {
@@ -384,7 +391,8 @@ template <int DT> __global__ void __launch_bounds__(256) attn_dkv_join_kernel(At
 }
 
 // Pieces of the queries of a key tile: few key heads and short batches leave most compute units idle otherwise (one sequence of 1000 keys with one head
-// is eight workgroups). An estimate in microseconds as for the forward: a step of a workgroup takes 2 at d = 128 with the chip full, its start 5.
+// is eight workgroups: all gradients 304 us, 64 in the pieces chosen here). An estimate in microseconds: a step of a workgroup takes 2 at d = 128
+// with the chip full, its start 5, joining a launch and a round trip of fp32 sums.
 int dkv_pieces(int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, int hkv, int d, int num_cu)
 {
     const double full = 2.0 * num_cu, work = (double)(k_tokens / (NK * 32) + b) * hkv, steps = std::max(1.0, (double)q_tokens / b / Q_TILE) * (hq / hkv);
