@@ -79,6 +79,29 @@ def test_few_queries_many_keys(b, lq, lk, hq, hkv, d):
         compare((b, lq, lk, causal), *inputs([lq] * b, [lk - 17 * i for i in range(b)], hq, hkv, d, "bf16"), causal)
 
 
+@pytest.mark.parametrize("q,k,hq,hkv,d,dtype", [
+    ([1, 1, 1, 2, 1], [24000, 1, 0, 700, 333], 32, 8, 128, "bf16"),
+    ([1] * 5, [8000, 8001, 8191, 33, 8500], 8, 8, 96, "f16"),
+    ([2, 3, 1], [20000, 13001, 64], 12, 12, 64, "f16"),
+    ([1], [50000], 16, 16, 32, "bf16"),
+    ([1, 0, 1], [6000, 9000, 29000], 16, 8, 72, "bf16"),
+    ([4, 1], [12000, 700], 16, 8, 256, "f16"),
+    ([1, 1], [65537, 131000], 32, 1, 128, "f16"),
+    ([30], [24500], 8, 8, 128, "bf16"),
+])
+def test_few_queries_large_caches(q, k, hq, hkv, d, dtype):
+    """From 100 MB of keys and values on they stream past the caches, to a wavefront of its own for every second tile."""
+    assert sum(k) * hkv * d * 4 >= 1e8 and sum(q) * (hq // hkv) <= 32 * len(q)
+    Q, K, V, _, qo, ko = inputs(q, k, hq, hkv, d, dtype)
+    for causal in (True, False):
+        print(q, k, hq, hkv, d, dtype, causal, flush=True)
+        O, lse = M.maxsim_attention(Q, K, V, qo, ko, causal=causal)
+        torch.cuda.synchronize()
+        want = R.attention(Q, K, V, qo, ko, causal, d ** -0.5)
+        R.check("O", O, want["O"])
+        R.check("lse", lse, want["lse"])
+
+
 @pytest.mark.parametrize("lens,hq,hkv,d", [([1000], 8, 1, 128), ([700, 33], 6, 2, 80), ([2000], 1, 1, 64), ([129, 0, 1500], 16, 1, 32), ([700, 5], 8, 1, 256)])
 def test_few_key_heads(lens, hq, hkv, d):
     """Where the queries of a key tile are taken in pieces for dK and dV."""
