@@ -200,7 +200,7 @@ template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, DP 
 // rate. A wavefront owns all 32 rows of the workgroup and every NF-th tile of 32 keys of the piece, which it copies to a ring in
 // LDS of its own, RING tiles of K and of V ahead: nothing waits for another wavefront, and two workgroups keep 100 KB on their way to a compute
 // unit. The wavefronts' results are joined through LDS at the end. Bound by the memory: one token after each of 64 x 2048 .. 8192 keys, 8
-// heads of 128 (1.4 GB), 245 us, 5.9 TB/s; one token after 100003 keys of two heads (102 MB) 20 us and 7 for the join.
+// heads of 128 (1.4 GB), 245 us, 5.9 TB/s; one token after 100003 keys of two heads (102 MB) 20.7 us and 6 for the join.
 // Workgroups go round the XCDs one by one: in contiguous ranges, as in the other kernel, unequal sequences load the XCDs unequally
 // (16 sequences of 500 .. 16000 keys 117 us, 87 so; 32 x 4000 keys of 16 heads 181 and 164).
 constexpr int NF = 2;
@@ -378,15 +378,25 @@ template <int DT, int PIECES> __global__ void __launch_bounds__(256) attn_join_k
         for (int m = 32; m; m >>= 1)
             top = fmaxf(top, __shfl_xor(top, m, 64));
     }
-#pragma unroll 4
-    for (int s = g; s < p.n_split; s += PIECES) {
-        const float by = __builtin_amdgcn_exp2f((lse[s * n] - top) * 1.44269504088896341f);
-        const float4 y = *reinterpret_cast<const float4 *>(p.part_o + (s * n + at) * p.d + e);
-        sum += by;
-        o[0] = __builtin_fmaf(by, y.x, o[0]);
-        o[1] = __builtin_fmaf(by, y.y, o[1]);
-        o[2] = __builtin_fmaf(by, y.z, o[2]);
-        o[3] = __builtin_fmaf(by, y.w, o[3]);
+    constexpr int AT_ONCE = PIECES == 1 ? 4 : 8; // loads on their way; past the last piece it is read again, for nothing
+    for (int s0 = g; s0 < p.n_split; s0 += PIECES * AT_ONCE) {
+        float l[AT_ONCE];
+        float4 y[AT_ONCE];
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+            const int s = min(s0 + i * PIECES, p.n_split - 1);
+            l[i] = lse[s * n];
+            y[i] = *reinterpret_cast<const float4 *>(p.part_o + (s * n + at) * p.d + e);
+        }
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+            const float by = s0 + i * PIECES < p.n_split ? __builtin_amdgcn_exp2f((l[i] - top) * 1.44269504088896341f) : 0.0f;
+            sum += by;
+            o[0] = __builtin_fmaf(by, y[i].x, o[0]);
+            o[1] = __builtin_fmaf(by, y[i].y, o[1]);
+            o[2] = __builtin_fmaf(by, y[i].z, o[2]);
+            o[3] = __builtin_fmaf(by, y[i].w, o[3]);
+        }
     }
 #pragma unroll
     for (int m = 8; m < 8 * PIECES; m <<= 1) {
@@ -431,7 +441,7 @@ AttnPlan attn_plan(int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, int hk
     // if it has the compute unit for itself and 1.5 beside another one; the memory gives 6.4 TB/s, and pieces of unequal sequences end at
     // different times; joining takes a launch and a round trip of fp32 results. Over 28 shapes of one to 500 new tokens, 1 to 200
     // sequences and 500 to 131072 keys, equal and ragged, the choice takes 3 % longer than the best number on average and 19 % at most: one
-    // token after 2000 keys of two heads 37 us in one piece, 11.7 in 12; 100 tokens after 8192 keys 141 and 27 (23 in 16 pieces).
+    // token after 2000 keys of two heads 37 us in one piece, 10.8 in 12; 100 tokens after 8192 keys 141 and 27 (23 in 16 pieces).
     const double full = 2.0 * num_cu, wgs = (double)((q_tokens * x.pack + b * rows - 1) / (b * rows)) * b * hkv, tiles = std::max(1.0, (double)k_tokens / b / 64);
     const double width = (d + 32) / 160.0, join = (double)q_tokens * hq * d * 8 / 6.0e6;
     double best = 0;
