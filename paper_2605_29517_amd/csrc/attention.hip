@@ -506,8 +506,8 @@ hipError_t attention_launch(AttnParams p, int dtype, void *workspace, int num_cu
         else
             attn_join_kernel<MAXSIM_BF16, PIECES><<<wgs, 256, 0, stream>>>(p);
     };
-    // 16 pieces of 256 rows of 128 (1024 units) 19.0 us with a group for a row's pieces, 13.6 with eight; of 4800 rows (19200) 46.8 and 46.5,
-    // 6 pieces of those 39.1 and 42.3, 6 of 100 rows 35.5 and 35.7
+    // 16 pieces of 32 rows of 128 (128 units) 19.0 us with a group for a row's pieces, 13.6 with eight; of 4800 rows (19200) 46.8 and 46.5,
+    // 6 pieces of those 39.1 and 42.3, 6 of 1600 rows (6400) 35.5 and 35.7
     if (x.n_split < (units > 8192 ? 16 : 6))
         join(std::integral_constant<int, 1>{});
     else
