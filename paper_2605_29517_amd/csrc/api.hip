@@ -194,6 +194,8 @@ int attention_common(maxsim::AttnParams &p, const AttnTensor *t, int n, const in
     p.hq = hq;
     p.hkv = hkv;
     p.d = d;
+    // (the same offsets over other numbers of rows are cut to each side's own, as any offsets are: no row is read that is not there)
+    p.same = q_offsets == k_offsets && q_tokens == k_tokens;
     p.causal = causal != 0;
     p.scale = scale;
     p.scale_log2 = scale * 1.44269504088896341f;

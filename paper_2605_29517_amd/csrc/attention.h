@@ -53,6 +53,7 @@ struct AttnParams {
     int n_slots; // see attn_find_slot
     int n_split; // pieces of the keys
     AttnDivisor by_pack, by_slots, by_split, by_hkv;
+    int same; // queries and keys have the same rows: one pair of offsets to read
     int causal;
     float scale, scale_log2; // scale_log2 = scale * log2(e)
 };

@@ -66,7 +66,7 @@ template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, DP 
     const int piece = v, hk = p.by_slots(u), slot = p.n_slots - 1 - u;
 
     const AttnPlace place = attn_find_slot<ROWS>(p.q_off, p.b, p.q_tokens, p.pack, slot, p.n_slots);
-    const AttnSeq q = place.s, k = p.k_off == p.q_off ? q : attn_seq(p.k_off, place.i, p.k_tokens);
+    const AttnSeq q = place.s, k = p.same ? q : attn_seq(p.k_off, place.i, p.k_tokens);
     const int first = (slot - place.first) * ROWS, rows = q.len * p.pack;
     if (first < 0 || first >= rows)
         return;
@@ -217,7 +217,7 @@ template <int DT, int DP> __global__ void __launch_bounds__(NF * 64, 1) attn_few
     const int hk = v, slot = p.by_split(u), piece = u;
 
     const AttnPlace place = attn_find_slot<32>(p.q_off, p.b, p.q_tokens, p.pack, slot, p.n_slots);
-    const AttnSeq q = place.s, k = p.k_off == p.q_off ? q : attn_seq(p.k_off, place.i, p.k_tokens);
+    const AttnSeq q = place.s, k = p.same ? q : attn_seq(p.k_off, place.i, p.k_tokens);
     const int first = (slot - place.first) * 32, rows = q.len * p.pack;
     if (first < 0 || first >= rows)
         return;

@@ -39,7 +39,7 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, DP > 128 ? 
     const int hk = p.by_slots(v), slot = p.n_slots - 1 - v;
 
     const AttnPlace place = attn_find_slot<ROWS>(p.q_off, p.b, p.q_tokens, p.pack, slot, p.n_slots);
-    const AttnSeq q = place.s, k = p.k_off == p.q_off ? q : attn_seq(p.k_off, place.i, p.k_tokens);
+    const AttnSeq q = place.s, k = p.same ? q : attn_seq(p.k_off, place.i, p.k_tokens);
     const int first = (slot - place.first) * ROWS, rows = q.len * p.pack;
     if (first < 0 || first >= rows)
         return;
@@ -217,7 +217,7 @@ template <int DT, int DP> __global__ void __launch_bounds__(NK * 64, DP > 128 ? 
     const int piece = v, hk = p.by_slots(x), slot = x;
 
     const AttnPlace place = attn_find_slot<KEYS>(p.k_off, p.b, p.k_tokens, 1, slot, p.n_slots);
-    const AttnSeq k = place.s, q = p.k_off == p.q_off ? k : attn_seq(p.q_off, place.i, p.q_tokens);
+    const AttnSeq k = place.s, q = p.same ? k : attn_seq(p.q_off, place.i, p.q_tokens);
     const int first = (slot - place.first) * KEYS, ahead = k.len - q.len;
     if (first < 0 || first >= k.len)
         return;

@@ -1,0 +1,44 @@
+"""maxsim_attention and maxsim_attention_backward where sizes, layouts and numbers are at their ends."""
+import math
+import os
+import sys
+
+import pytest
+import torch
+
+from paper_2605_29517_amd import binding as M
+
+sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
+import attention_reference as R  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"f16": torch.float16, "bf16": torch.bfloat16}
+
+
+def inputs(q_lens, k_lens, hq, hkv, d, dtype, seed=0, by=2.0):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    make = lambda t, h, x=1.0: (torch.randn(t, h, d, generator=g, device=DEV) * x).to(TYPES[dtype])  # noqa: E731
+    tq, tk = sum(q_lens), sum(k_lens)
+    return make(tq, hq, by), make(tk, hkv), make(tk, hkv), make(tq, hq), R.offsets(q_lens, DEV), R.offsets(k_lens, DEV)
+
+
+def run(Q, K, V, dO, qo, ko, causal):
+    O, lse = M.maxsim_attention(Q, K, V, qo, ko, causal=causal)
+    grads = M.maxsim_attention_backward(Q, K, V, O, lse, dO, qo, ko, causal=causal)
+    torch.cuda.synchronize()
+    return dict(zip(("O", "lse", "dQ", "dK", "dV"), (O, lse, *grads)))
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("tq,tk", [(150, 100), (150, 60), (100, 150), (60, 150)])
+def test_one_offset_array_over_other_numbers_of_rows(tq, tk, causal):
+    """The same memory as both offsets, though Q and K have not the same rows: each side's sequences end where its rows do, as with two arrays."""
+    print(tq, tk, causal, flush=True)
+    lens = [40, 60, 50]
+    Q, K, V, dO, off, _ = inputs(lens, lens, 2, 1, 64, "bf16")
+    got = run(Q[:tq].clone(), K[:tk].clone(), V[:tk].clone(), dO[:tq].clone(), off, off.view(-1), causal)
+    want = R.attention(Q[:tq], K[:tk], V[:tk], off.clamp(max=tq), off.clamp(max=tk), causal, 64 ** -0.5, dO[:tq])
+    for name in want:
+        R.check(name, got[name], want[name])
