@@ -52,6 +52,7 @@ struct AttnParams {
     int pack;
     int n_slots; // see attn_find_slot
     int n_split; // pieces of the keys
+    int n_wg;    // workgroups that the launch is for
     AttnDivisor by_pack, by_slots, by_split, by_hkv;
     int same; // queries and keys have the same rows: one pair of offsets to read
     int causal;

@@ -62,7 +62,10 @@ template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, DP 
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // Every XCD takes a contiguous range of (kv head, tile, piece): tiles that read the same keys meet in one L2 (prompt of 8192 tokens
     // 538 us, tile by tile over all heads 955). The last tiles, which see the most keys under a causal mask, come first.
-    int v = xcd_grouped(blockIdx.x, gridDim.x), u = p.by_split(v);
+    const int wg = blockIdx.y * (int)GRID_ROW + blockIdx.x;
+    if (wg >= p.n_wg)
+        return;
+    int v = xcd_grouped(wg, p.n_wg), u = p.by_split(v);
     const int piece = v, hk = p.by_slots(u), slot = p.n_slots - 1 - u;
 
     const AttnPlace place = attn_find_slot<ROWS>(p.q_off, p.b, p.q_tokens, p.pack, slot, p.n_slots);
@@ -213,7 +216,10 @@ template <int DT, int DP> __global__ void __launch_bounds__(NF * 64, 1) attn_few
     const int lane = threadIdx.x & 63, h = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // (the heads of a piece, whose rows lie side by side, run at the same time)
-    int v = blockIdx.x, u = p.by_hkv(v);
+    int v = blockIdx.y * (int)GRID_ROW + blockIdx.x;
+    if (v >= p.n_wg)
+        return;
+    int u = p.by_hkv(v);
     const int hk = v, slot = p.by_split(u), piece = u;
 
     const AttnPlace place = attn_find_slot<32>(p.q_off, p.b, p.q_tokens, p.pack, slot, p.n_slots);
@@ -361,7 +367,7 @@ template <int DT, int PIECES> __global__ void __launch_bounds__(256) attn_join_k
     const int64_t n = (int64_t)p.q_tokens * p.hq;
     const int blocks = (p.d + 31) / 32;
     const int group = threadIdx.x >> 3, g = group % PIECES;
-    const int64_t unit = (int64_t)blockIdx.x * (32 / PIECES) + group / PIECES;
+    const int64_t unit = ((int64_t)blockIdx.y * GRID_ROW + blockIdx.x) * (32 / PIECES) + group / PIECES;
     const bool in = unit < n * blocks;
     const int64_t at = in ? unit / blocks : 0;
     const int e = min((int)(unit % blocks) * 32 + (int)(threadIdx.x & 7) * 4, p.d - 4); // (past the row's end: its last four again)
@@ -480,7 +486,8 @@ hipError_t attention_launch(AttnParams p, int dtype, void *workspace, int num_cu
     p.by_slots = AttnDivisor::of(x.n_slots);
     p.by_split = AttnDivisor::of(x.n_split);
     p.by_hkv = AttnDivisor::of(p.hkv);
-    const unsigned grid = (unsigned)(x.n_slots * p.hkv * x.n_split);
+    p.n_wg = x.n_slots * p.hkv * x.n_split;
+    const dim3 grid = grid_rows(p.n_wg);
     const hipError_t e = attn_width(p.d, [&](auto dp) {
         constexpr int DP = decltype(dp)::value;
         if (x.few) {
@@ -500,7 +507,7 @@ hipError_t attention_launch(AttnParams p, int dtype, void *workspace, int num_cu
     const int64_t units = (int64_t)p.q_tokens * p.hq * ((p.d + 31) / 32);
     auto join = [&](auto pieces) {
         constexpr int PIECES = decltype(pieces)::value;
-        const unsigned wgs = (unsigned)((units * PIECES + 31) / 32);
+        const dim3 wgs = grid_rows((units * PIECES + 31) / 32);
         if (dtype == MAXSIM_F16)
             attn_join_kernel<MAXSIM_F16, PIECES><<<wgs, 256, 0, stream>>>(p);
         else

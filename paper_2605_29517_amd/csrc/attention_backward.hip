@@ -35,7 +35,10 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, DP > 128 ? 
 
     const int lane = threadIdx.x & 63, h = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    int v = xcd_grouped(blockIdx.x, gridDim.x); // (as in the forward)
+    const int wg = blockIdx.y * (int)GRID_ROW + blockIdx.x;
+    if (wg >= p.n_wg)
+        return;
+    int v = xcd_grouped(wg, p.n_wg); // (as in the forward)
     const int hk = p.by_slots(v), slot = p.n_slots - 1 - v;
 
     const AttnPlace place = attn_find_slot<ROWS>(p.q_off, p.b, p.q_tokens, p.pack, slot, p.n_slots);
@@ -200,20 +203,23 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, DP > 128 ? 
 
 // NK: wavefronts of 32 keys, which share the tiles of queries; the gradient of 4 x 4096 causal tokens, 32 heads of 128 over 8, took 2626 us with one, 2091 with two, 1997
 // with four and 2037 with eight.
-// A wavefront owns 32 keys (columns) of one key head; at d = 256 the registers hold the gradients of half of d, and blockIdx.y says which.
+// A wavefront owns 32 keys (columns) of one key head; at d = 256 the registers hold the gradients of half of d, and blockIdx.z says which.
 constexpr int NK = 4;
 constexpr int dkv_slices(int dp) { return dp > 128 ? 2 : 1; }
 constexpr int dkv_buffer(int dp) { return 2 * Q_TILE * dp * 2 + 256; } // Q, dO, 32 of -lse / scale, 32 of -delta
 template <int DT, int DP> __global__ void __launch_bounds__(NK * 64, DP > 128 ? 1 : DP > 64 ? 2 : 3) attn_dkv_kernel(AttnParams p)
 {
     constexpr int KEYS = NK * 32, U = DP / 16, SLICES = dkv_slices(DP), SLICE = DP / SLICES, NB = SLICE / 32, C = 2 * NB;
-    const int slice = SLICES > 1 ? blockIdx.y : 0;
+    const int slice = SLICES > 1 ? blockIdx.z : 0;
     constexpr int TILE_BYTES = Q_TILE * DP * 2, BUF = dkv_buffer(DP);
     extern __shared__ __attribute__((aligned(16))) char lds[]; // two buffers
 
     const int lane = threadIdx.x & 63, h = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    int v = xcd_grouped(blockIdx.x, gridDim.x), x = p.by_split(v); // (the first tiles, which the most queries see under a causal mask, come first)
+    const int wg = blockIdx.y * (int)GRID_ROW + blockIdx.x;
+    if (wg >= p.n_wg)
+        return;
+    int v = xcd_grouped(wg, p.n_wg), x = p.by_split(v); // (the first tiles, which the most queries see under a causal mask, come first)
     const int piece = v, hk = p.by_slots(x), slot = x;
 
     const AttnPlace place = attn_find_slot<KEYS>(p.k_off, p.b, p.k_tokens, 1, slot, p.n_slots);
@@ -373,7 +379,7 @@ template <int DT, int DP> __global__ void __launch_bounds__(NK * 64, DP > 128 ? 
 // Adds the pieces up, in their order; a thread per four entries of a row
 template <int DT> __global__ void __launch_bounds__(256) attn_dkv_join_kernel(AttnParams p)
 {
-    const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x, n = (int64_t)p.k_tokens * p.hkv * p.d;
+    const int64_t x = ((int64_t)blockIdx.y * GRID_ROW + blockIdx.x) * 256 + threadIdx.x, n = (int64_t)p.k_tokens * p.hkv * p.d;
     if (x * 4 >= n)
         return;
     float4 k = make_float4(0.0f, 0.0f, 0.0f, 0.0f), v = k;
@@ -438,13 +444,18 @@ hipError_t attention_backward_launch(AttnParams p, int dtype, void *workspace, i
         constexpr int DP = decltype(dp)::value;
         p.n_slots = p.q_tokens * p.pack / (NW * 32) + p.b;
         p.by_slots = AttnDivisor::of(p.n_slots);
+        p.n_wg = p.n_slots * p.hkv;
         if (dtype == MAXSIM_F16)
-            attn_dq_kernel<MAXSIM_F16, DP><<<(unsigned)(p.n_slots * p.hkv), NW * 64, 0, stream>>>(p);
+            attn_dq_kernel<MAXSIM_F16, DP><<<grid_rows(p.n_wg), NW * 64, 0, stream>>>(p);
         else
-            attn_dq_kernel<MAXSIM_BF16, DP><<<(unsigned)(p.n_slots * p.hkv), NW * 64, 0, stream>>>(p);
+            attn_dq_kernel<MAXSIM_BF16, DP><<<grid_rows(p.n_wg), NW * 64, 0, stream>>>(p);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) // (nothing reads row statistics that have not been written)
+            return e;
         p.n_slots = p.k_tokens / (NK * 32) + p.b;
         p.by_slots = AttnDivisor::of(p.n_slots);
-        const dim3 grid((unsigned)(p.n_slots * p.hkv * p.n_split), dkv_slices(DP));
+        p.n_wg = p.n_slots * p.hkv * p.n_split;
+        dim3 grid = grid_rows(p.n_wg);
+        grid.z = dkv_slices(DP);
         if (dtype == MAXSIM_F16)
             attn_dkv_kernel<MAXSIM_F16, DP><<<grid, NK * 64, 2 * dkv_buffer(DP), stream>>>(p);
         else
@@ -453,7 +464,7 @@ hipError_t attention_backward_launch(AttnParams p, int dtype, void *workspace, i
     });
     if (e != hipSuccess || p.n_split == 1)
         return e;
-    const unsigned join = (unsigned)(((int64_t)p.k_tokens * p.hkv * p.d / 4 + 255) / 256);
+    const dim3 join = grid_rows(((int64_t)p.k_tokens * p.hkv * p.d / 4 + 255) / 256);
     if (dtype == MAXSIM_F16)
         attn_dkv_join_kernel<MAXSIM_F16><<<join, 256, 0, stream>>>(p);
     else

@@ -238,6 +238,12 @@ __device__ __forceinline__ int xcd_grouped(unsigned id, unsigned n)
     return (int)(xcd * (n >> 3) + (xcd < (n & 7) ? xcd : n & 7) + (id >> 3));
 }
 
+// One dimension of a grid holds less than 2^32 threads; what is beyond is cut off without an error. n workgroups of up to 256 threads as a
+// grid of one row or, of more than GRID_ROW, of rows of GRID_ROW (a multiple of the XCDs): workgroup id is blockIdx.y * GRID_ROW +
+// blockIdx.x, and those from n on have nothing to do.
+constexpr int64_t GRID_ROW = int64_t(1) << 22;
+inline dim3 grid_rows(int64_t n) { return n <= GRID_ROW ? dim3((unsigned)n) : dim3((unsigned)GRID_ROW, (unsigned)((n + GRID_ROW - 1) / GRID_ROW)); }
+
 // Documents [doc0, doc1) of work chunk `chunk`.  Uniform corpus: equal document counts.
 // Ragged corpus: the packed token range is cut into equal pieces and a chunk owns every
 // document that starts inside its piece (binary search over the offsets).

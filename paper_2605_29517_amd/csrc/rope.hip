@@ -78,7 +78,9 @@ template <int DT, int V, RopePairs PAIRS, bool ONCE> __global__ void __launch_bo
     constexpr int SIZE = sizeof(T);
     __shared__ float2 table[MAX_TABLE];
     const int half = p.rot / 2;
-    const int64_t token0 = (int64_t)blockIdx.x * p.per_wg;
+    const int64_t token0 = ((int64_t)blockIdx.y * GRID_ROW + blockIdx.x) * p.per_wg;
+    if (token0 >= p.tokens)
+        return;
     const int n = (int)(p.tokens - token0 < p.per_wg ? p.tokens - token0 : p.per_wg);
 
     int64_t seq0 = 0, seq1 = 0; // the first sequences that start after the first and after the last token
@@ -204,7 +206,7 @@ template <int DT, bool ONCE> void launch(RopeParams p, bool wide, hipStream_t st
     while (per > 1 && p.tokens / per < 2048)
         per /= 2;
     p.per_wg = (int)std::min<int64_t>(per, MAX_TABLE / std::max(1, half));
-    const unsigned grid = (unsigned)((p.tokens + p.per_wg - 1) / p.per_wg);
+    const dim3 grid = grid_rows((p.tokens + p.per_wg - 1) / p.per_wg);
     if (pairs == SINGLE)
         rope_kernel<DT, 1, SINGLE, false><<<grid, WG, 0, stream>>>(p);
     else if (pairs == NEIGHBOURS)

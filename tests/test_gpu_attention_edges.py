@@ -42,3 +42,21 @@ def test_one_offset_array_over_other_numbers_of_rows(tq, tk, causal):
     want = R.attention(Q[:tq], K[:tk], V[:tk], off.clamp(max=tq), off.clamp(max=tk), causal, 64 ** -0.5, dO[:tq])
     for name in want:
         R.check(name, got[name], want[name])
+
+
+def test_more_sequences_than_one_grid_dimension_takes():
+    """2^19 sequences of one token, 40 heads: 21 million workgroups of 256 threads, more than 2^32 threads. One key: O = V, lse = the score, dV = dO and
+    no other gradient."""
+    b, heads, d = 1 << 19, 40, 8
+    print(b, heads, d, flush=True)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1)
+    Q, K, V, dO = (torch.randn(b, heads, d, generator=g, device=DEV, dtype=torch.float16) for _ in range(4))
+    off = torch.arange(b + 1, dtype=torch.int32, device=DEV)
+    O, lse = M.maxsim_attention(Q, K, V, off)
+    dQ, dK, dV = M.maxsim_attention_backward(Q, K, V, O, lse, dO, off)
+    torch.cuda.synchronize()
+    assert torch.equal(O, V) and torch.equal(dV, dO)
+    score = (Q.float() * K.float()).sum(-1) * d ** -0.5
+    assert ((lse - score).abs() <= 2.0 ** -20 * (1 + (Q.float() * K.float()).abs().sum(-1))).all()
+    assert dQ.abs().max() <= 2.0 ** -9 and dK.abs().max() <= 2.0 ** -9
