@@ -15,10 +15,10 @@ namespace {
 constexpr float NO_MAXIMUM = -1.0e30f;  // of a row that has seen no key: finite, so that no difference of infinities arises
 constexpr float LAZY = 8.0f;            // the maximum may lag by this many powers of two: P <= 2^8, far from overflow in fp16
 
-// A column's result: O = o / sum and lse, or the same of a piece
-template <int DT, int NB> __device__ __forceinline__ void attn_write(const AttnParams &p, const f32x16 (&o)[NB], float top, float sum, int piece, int token, int head, int h)
+// A column's result: O = o / sum and lse, or the same of a piece. `seen`: that there is a key, which the mask says and not the sum, so that a sum which
+// is not a number shows in lse (with NaNs not honoured by the compiler a comparison of it would say anything).
+template <int DT, int NB> __device__ __forceinline__ void attn_write(const AttnParams &p, const f32x16 (&o)[NB], float top, float sum, bool seen, int piece, int token, int head, int h)
 {
-    const bool seen = sum > 0.0f;
     const float by = seen ? 1.0f / sum : 0.0f;
     const float lse = seen ? (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f : neg_inf();
     const int at = token * p.hq + head;
@@ -185,11 +185,11 @@ template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, DP 
     sum = attn_halves_sum(sum);
     if (p.n_split > 1) {
         if (row < rows)
-            attn_write<DT>(p, o, top, sum, piece, q.start + token, head, h);
+            attn_write<DT>(p, o, top, sum, limit > t0 * TILE, piece, q.start + token, head, h);
         return;
     }
     __syncthreads(); // (nobody reads the tiles any more)
-    const bool seen = sum > 0.0f;
+    const bool seen = limit > 0; // (as in attn_write)
     attn_store_tile<DT, DP>(lds + w * 32 * DP * 2, o, seen ? 1.0f / sum : 0.0f, lane, p.d, rows - first - w * 32, [&](int r) {
         int g = first + w * 32 + r;
         const uint32_t t = q.start + p.by_pack(g);
@@ -355,7 +355,7 @@ template <int DT, int DP> __global__ void __launch_bounds__(NF * 64, 1) attn_few
                 o[b][r] = o[b][r] * by + theirs[(b * 16 + r) * 64] * by2;
     }
     if (row < rows)
-        attn_write<DT>(p, o, top, sum, piece, q.start + token, head, h);
+        attn_write<DT>(p, o, top, sum, limit > start * KEYS, piece, q.start + token, head, h);
 }
 
 // Joins the pieces of a row: weights exp(lse_piece - lse). Eight lanes read 128 bytes of a piece; PIECES such groups, 1 or the 8 of a wavefront,
@@ -415,12 +415,13 @@ template <int DT, int PIECES> __global__ void __launch_bounds__(256) attn_join_k
         return;
     if (!in)
         return;
-    const float by = sum > 0.0f ? 1.0f / sum : 0.0f;
+    const bool seen = __float_as_uint(sum) != 0; // (by its bits: a piece that is not a number makes the sum one)
+    const float by = seen ? 1.0f / sum : 0.0f;
     const int64_t token = at / p.hq;
     const int head = (int)(at % p.hq);
     attn_store4<DT>(p.O.p + token * p.O.token + head * p.O.head, e, o[0] * by, o[1] * by, o[2] * by, o[3] * by);
     if (p.lse && e == 0)
-        p.lse[at] = sum > 0.0f ? top + __builtin_amdgcn_logf(sum) * 0.69314718055994531f : neg_inf();
+        p.lse[at] = seen ? top + __builtin_amdgcn_logf(sum) * 0.69314718055994531f : neg_inf();
 }
 
 struct AttnPlan {

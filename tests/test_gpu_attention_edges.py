@@ -60,3 +60,24 @@ def test_more_sequences_than_one_grid_dimension_takes():
     score = (Q.float() * K.float()).sum(-1) * d ** -0.5
     assert ((lse - score).abs() <= 2.0 ** -20 * (1 + (Q.float() * K.float()).abs().sum(-1))).all()
     assert dQ.abs().max() <= 2.0 ** -9 and dK.abs().max() <= 2.0 ** -9
+
+
+@pytest.mark.parametrize("name,q,k,hq,hkv,d,bad_key", [
+    ("whole tiles", [70, 90, 200], [70, 90, 200], 4, 2, 64, 75),
+    ("pieces", [1, 2], [20011, 3000], 4, 1, 128, 20000),
+    ("streamed", [1, 1, 1], [30000, 9000, 11000], 8, 8, 64, 30500),
+])
+def test_lse_shows_what_is_not_a_number(name, q, k, hq, hkv, d, bad_key):
+    """A key that is not a number makes lse of the rows that see it one that is not either: never -inf, which says that a row sees no key, and never
+    the finite one of the other keys."""
+    Q, K, V, _, qo, ko = inputs(q, k, hq, hkv, d, "bf16")
+    print(name, flush=True)
+    want = M.maxsim_attention(Q, K, V, qo, ko, causal=False)
+    K[bad_key] = float("nan")
+    got = M.maxsim_attention(Q, K, V, qo, ko, causal=False)
+    torch.cuda.synchronize()
+    s = int(torch.searchsorted(ko, bad_key, right=True)) - 1
+    rows = torch.zeros(sum(q), dtype=torch.bool, device=DEV)
+    rows[int(qo[s]):int(qo[s + 1])] = True
+    assert torch.equal(got[1][~rows], want[1][~rows]) and torch.equal(got[0][~rows], want[0][~rows])
+    assert got[1][rows].isnan().all() and got[0][rows].isnan().all()
