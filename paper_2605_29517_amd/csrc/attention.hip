@@ -12,15 +12,22 @@
 namespace maxsim {
 namespace {
 
-constexpr float NO_MAXIMUM = -1.0e30f;  // of a row that has seen no key: finite, so that no difference of infinities arises
+constexpr float NO_MAXIMUM = -3.4028234664e38f; // of a row that has seen no key, the lowest finite number, so that no difference of infinities arises
 constexpr float LAZY = 8.0f;            // the maximum may lag by this many powers of two: P <= 2^8, far from overflow in fp16
+// P = exp2(scale_log2 S - scale_log2 top) by one fma, with top among the scores S as they are. The fma's product is exact and the number that it
+// subtracts is rounded, so that all of a row's P are off by one factor, which the sum that divides them shares: 2^-4 of an exponent at
+// FAR, but more than P can hold from 2^28 on. Further out than FAR the difference is taken first: scores of +-10^38 (bf16) are told apart as fp32 tells them.
+constexpr float FAR = 1048576.0f;
+
+// Of a row that sees keys
+__device__ __forceinline__ float attn_lse(const AttnParams &p, float top, float sum) { return __builtin_fmaf(top, p.scale, __builtin_amdgcn_logf(sum) * 0.69314718055994531f); }
 
 // A column's result: O = o / sum and lse, or the same of a piece. `seen`: that there is a key, which the mask says and not the sum, so that a sum which
 // is not a number shows in lse (with NaNs not honoured by the compiler a comparison of it would say anything).
-template <int DT, int NB> __device__ __forceinline__ void attn_write(const AttnParams &p, const f32x16 (&o)[NB], float top, float sum, bool seen, int piece, int token, int head, int h)
+template <int DT, int NB> __device__ __forceinline__ void attn_write(const AttnParams &p, const f32x16 (&o)[NB], float lse, float sum, bool seen, int piece, int token, int head, int h)
 {
     const float by = seen ? 1.0f / sum : 0.0f;
-    const float lse = seen ? (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f : neg_inf();
+    lse = seen ? lse : neg_inf();
     const int at = token * p.hq + head;
     if (p.n_split > 1) {
         float *part = p.part_o + ((int64_t)piece * (p.q_tokens * p.hq) + at) * p.d;
@@ -136,10 +143,10 @@ template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, DP 
 #pragma unroll
             for (int r = 0; r < 16; ++r)
                 m = fmaxf(m, s[b][r]);
-        m = attn_halves_max(m) * p.scale_log2;
+        m = attn_halves_max(m);
         // A maximum that grows by less than 2^LAZY is left where it is (the result is the same whatever number is subtracted)
-        if (__builtin_amdgcn_ballot_w64(m > top + LAZY)) {
-            const float to = fmaxf(m, top), by = __builtin_amdgcn_exp2f(top - to);
+        if (__builtin_amdgcn_ballot_w64((m - top) * p.scale_log2 > LAZY)) {
+            const float to = fmaxf(m, top), by = __builtin_amdgcn_exp2f((top - to) * p.scale_log2);
             top = to;
             sum *= by;
 #pragma unroll
@@ -148,11 +155,20 @@ template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, DP 
                 for (int r = 0; r < 16; ++r)
                     o[b][r] *= by;
         }
+        float less = top * p.scale_log2;
+        if (__builtin_amdgcn_ballot_w64(fabsf(less) > FAR)) {
+            less = 0.0f;
+#pragma unroll
+            for (int b = 0; b < B; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    s[b][r] -= top;
+        }
 #pragma unroll
         for (int b = 0; b < B; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                s[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], p.scale_log2, -top));
+                s[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], p.scale_log2, -less));
                 sum += s[b][r];
             }
 #pragma unroll
@@ -185,7 +201,7 @@ template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, DP 
     sum = attn_halves_sum(sum);
     if (p.n_split > 1) {
         if (row < rows)
-            attn_write<DT>(p, o, top, sum, limit > t0 * TILE, piece, q.start + token, head, h);
+            attn_write<DT>(p, o, attn_lse(p, top, sum), sum, limit > t0 * TILE, piece, q.start + token, head, h);
         return;
     }
     __syncthreads(); // (nobody reads the tiles any more)
@@ -196,7 +212,7 @@ template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, DP 
         return p.O.p + (uint64_t)t * p.O.token + (hk * p.pack + g) * p.O.head;
     });
     if (p.lse && h == 0 && row < rows)
-        p.lse[(q.start + token) * p.hq + head] = seen ? (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f : neg_inf();
+        p.lse[(q.start + token) * p.hq + head] = seen ? attn_lse(p, top, sum) : neg_inf();
 }
 
 // The same for few rows per sequence (single tokens against kept keys): what counts is that keys and values stream at the memory's
@@ -290,9 +306,9 @@ template <int DT, int DP> __global__ void __launch_bounds__(NF * 64, 1) attn_few
 #pragma unroll
         for (int r = 1; r < 16; ++r)
             m = fmaxf(m, s[r]);
-        m = attn_halves_max(m) * p.scale_log2;
-        if (__builtin_amdgcn_ballot_w64(m > top + LAZY)) {
-            const float to = fmaxf(m, top), by = __builtin_amdgcn_exp2f(top - to);
+        m = attn_halves_max(m);
+        if (__builtin_amdgcn_ballot_w64((m - top) * p.scale_log2 > LAZY)) {
+            const float to = fmaxf(m, top), by = __builtin_amdgcn_exp2f((top - to) * p.scale_log2);
             top = to;
             sum *= by;
 #pragma unroll
@@ -301,9 +317,16 @@ template <int DT, int DP> __global__ void __launch_bounds__(NF * 64, 1) attn_few
                 for (int r = 0; r < 16; ++r)
                     o[b][r] *= by;
         }
+        float less = top * p.scale_log2;
+        if (__builtin_amdgcn_ballot_w64(fabsf(less) > FAR)) {
+            less = 0.0f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                s[r] -= top;
+        }
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], p.scale_log2, -top));
+            s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], p.scale_log2, -less));
             sum += s[r];
         }
         if (j + RING < n)
@@ -345,7 +368,7 @@ template <int DT, int DP> __global__ void __launch_bounds__(NF * 64, 1) attn_few
     for (int x = 1; x < NF; ++x) {
         const float *theirs = results + (x - 1) * RESULT + lane;
         const float top2 = theirs[NB * 16 * 64], sum2 = theirs[(NB * 16 + 1) * 64];
-        const float to = fmaxf(top, top2), by = __builtin_amdgcn_exp2f(top - to), by2 = __builtin_amdgcn_exp2f(top2 - to);
+        const float to = fmaxf(top, top2), by = __builtin_amdgcn_exp2f((top - to) * p.scale_log2), by2 = __builtin_amdgcn_exp2f((top2 - to) * p.scale_log2);
         top = to;
         sum = sum * by + sum2 * by2;
 #pragma unroll
@@ -355,7 +378,7 @@ template <int DT, int DP> __global__ void __launch_bounds__(NF * 64, 1) attn_few
                 o[b][r] = o[b][r] * by + theirs[(b * 16 + r) * 64] * by2;
     }
     if (row < rows)
-        attn_write<DT>(p, o, top, sum, limit > start * KEYS, piece, q.start + token, head, h);
+        attn_write<DT>(p, o, attn_lse(p, top, sum), sum, limit > start * KEYS, piece, q.start + token, head, h);
 }
 
 // Joins the pieces of a row: weights exp(lse_piece - lse). Eight lanes read 128 bytes of a piece; PIECES such groups, 1 or the 8 of a wavefront,

@@ -81,3 +81,25 @@ def test_lse_shows_what_is_not_a_number(name, q, k, hq, hkv, d, bad_key):
     rows[int(qo[s]):int(qo[s + 1])] = True
     assert torch.equal(got[1][~rows], want[1][~rows]) and torch.equal(got[0][~rows], want[0][~rows])
     assert got[1][rows].isnan().all() and got[0][rows].isnan().all()
+
+
+@pytest.mark.parametrize("lengths", [([40, 3], [40, 3]), ([1, 1], [9000, 700]), ([1], [110000])])
+@pytest.mark.parametrize("dtype,size", [("bf16", 2.0 ** 60), ("bf16", 2.0 ** 40), ("f16", 2.0 ** 15), ("f16", 2.0 ** 12)])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_scores_far_out(lengths, dtype, size, sign):
+    """Scores of up to +-10^36, where one key is ahead of all others by a factor: O is its V, lse its score. All scores of a row may be as low as the type goes."""
+    q, k = lengths
+    hq, hkv, d = 8, 4, 64
+    print(lengths, dtype, size, sign, flush=True)
+    _, _, V, dO, qo, ko = inputs(q, k, hq, hkv, d, dtype)
+    Q = torch.full((sum(q), hq, d), size, device=DEV, dtype=TYPES[dtype])
+    K = torch.full((sum(k), hkv, d), sign * size * 0.5, device=DEV, dtype=TYPES[dtype])
+    ahead = [int(a) + (int(n) * 2) // 3 for a, n in zip(ko, k)]
+    K[ahead] = sign * size * (1.0 if sign > 0 else 0.25)
+    O, lse = M.maxsim_attention(Q, K, V, qo, ko, causal=False)
+    torch.cuda.synchronize()
+    score = sign * size * size * (1.0 if sign > 0 else 0.25) * d * d ** -0.5
+    for s, at in enumerate(ahead):
+        rows = slice(int(qo[s]), int(qo[s + 1]))
+        assert torch.equal(O[rows], V[at].repeat_interleave(hq // hkv, 0).expand(O[rows].shape))
+        assert ((lse[rows].double() - score).abs() <= 2.0 ** -20 * abs(score)).all(), (lse[rows].flatten()[:4], score)
