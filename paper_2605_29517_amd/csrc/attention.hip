@@ -19,6 +19,39 @@ constexpr float LAZY = 8.0f;            // the maximum may lag by this many powe
 // FAR, but more than P can hold from 2^28 on. Further out than FAR the difference is taken first: scores of +-10^38 (bf16) are told apart as fp32 tells them.
 constexpr float FAR = 1048576.0f;
 
+// The softmax's sum, of which a row has up to millions of terms that may round alike (equal keys): a step's terms are added as a tree, and the steps with
+// what the last addition lost. Added one by one, 2^17 equal keys put lse 226 times as far
+// off as the rounding of the scores may; so it is half of that, for 1 % of the time of short texts (80.6 -> 81.7 us for 250 of them, long prompts 543 -> 545).
+struct AttnSum {
+    float sum, lost; // sum - lost is the value
+    __device__ __forceinline__ void add(float x)
+    {
+        const float y = x - lost, t = sum + y;
+        lost = (t - sum) - y;
+        sum = t;
+    }
+    __device__ __forceinline__ void scale(float by)
+    {
+        sum *= by;
+        lost *= by;
+    }
+};
+template <int N> __device__ __forceinline__ float attn_tree(const float *x)
+{
+    if constexpr (N == 1)
+        return x[0];
+    else
+        return attn_tree<N / 2>(x) + attn_tree<N - N / 2>(x + N / 2);
+}
+__device__ __forceinline__ float attn_tree(const f32x16 &x)
+{
+    float y[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+        y[r] = x[r];
+    return attn_tree<16>(y);
+}
+
 // Of a row that sees keys
 __device__ __forceinline__ float attn_lse(const AttnParams &p, float top, float sum) { return __builtin_fmaf(top, p.scale, __builtin_amdgcn_logf(sum) * 0.69314718055994531f); }
 
@@ -108,7 +141,8 @@ template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, DP 
 #pragma unroll
         for (int r = 0; r < 16; ++r)
             o[b][r] = 0.0f;
-    float top = NO_MAXIMUM, sum = 0.0f;
+    float top = NO_MAXIMUM;
+    AttnSum sums = {0.0f, 0.0f};
 
     const int tiles = (wg_keys + TILE - 1) / TILE;
     int over = tiles;
@@ -148,7 +182,7 @@ template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, DP 
         if (__builtin_amdgcn_ballot_w64((m - top) * p.scale_log2 > LAZY)) {
             const float to = fmaxf(m, top), by = __builtin_amdgcn_exp2f((top - to) * p.scale_log2);
             top = to;
-            sum *= by;
+            sums.scale(by);
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -167,10 +201,13 @@ template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, DP 
 #pragma unroll
         for (int b = 0; b < B; ++b)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
+            for (int r = 0; r < 16; ++r)
                 s[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], p.scale_log2, -less));
-                sum += s[b][r];
-            }
+        float part[B];
+#pragma unroll
+        for (int b = 0; b < B; ++b)
+            part[b] = attn_tree(s[b]);
+        sums.add(attn_tree<B>(part));
 #pragma unroll
         for (int b = 0; b < B; ++b)
 #pragma unroll
@@ -198,7 +235,7 @@ template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, DP 
                 step(kt + b * 32 * DP * 2, vt + b * 32 * DP * 2, key0 + 32 * b);
     }
 
-    sum = attn_halves_sum(sum);
+    const float sum = attn_halves_sum(sums.sum - sums.lost);
     if (p.n_split > 1) {
         if (row < rows)
             attn_write<DT>(p, o, attn_lse(p, top, sum), sum, limit > t0 * TILE, piece, q.start + token, head, h);
@@ -278,7 +315,8 @@ template <int DT, int DP> __global__ void __launch_bounds__(NF * 64, 1) attn_few
 #pragma unroll
         for (int r = 0; r < 16; ++r)
             o[b][r] = 0.0f;
-    float top = NO_MAXIMUM, sum = 0.0f;
+    float top = NO_MAXIMUM;
+    AttnSum sums = {0.0f, 0.0f};
     for (int j = 0; j < n; ++j) {
         const char *kt = ring + (j % RING) * 2 * TILE_BYTES, *vt = kt + TILE_BYTES;
         const int key0 = (t0 + NF * j) * KEYS;
@@ -310,7 +348,7 @@ template <int DT, int DP> __global__ void __launch_bounds__(NF * 64, 1) attn_few
         if (__builtin_amdgcn_ballot_w64((m - top) * p.scale_log2 > LAZY)) {
             const float to = fmaxf(m, top), by = __builtin_amdgcn_exp2f((top - to) * p.scale_log2);
             top = to;
-            sum *= by;
+            sums.scale(by);
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -325,10 +363,9 @@ template <int DT, int DP> __global__ void __launch_bounds__(NF * 64, 1) attn_few
                 s[r] -= top;
         }
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
+        for (int r = 0; r < 16; ++r)
             s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], p.scale_log2, -less));
-            sum += s[r];
-        }
+        sums.add(attn_tree(s));
         if (j + RING < n)
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"((2 * RING - 1) * LOADS) : "memory");
         else
@@ -344,7 +381,7 @@ template <int DT, int DP> __global__ void __launch_bounds__(NF * 64, 1) attn_few
         if (j + RING < n)
             issue_v(j + RING);
     }
-    sum = attn_halves_sum(sum);
+    float sum = attn_halves_sum(sums.sum - sums.lost);
 
     // the others' results, when nobody reads the rings any more
     constexpr int RESULT = (NB * 16 + 2) * 64;

@@ -103,3 +103,38 @@ def test_scores_far_out(lengths, dtype, size, sign):
         rows = slice(int(qo[s]), int(qo[s + 1]))
         assert torch.equal(O[rows], V[at].repeat_interleave(hq // hkv, 0).expand(O[rows].shape))
         assert ((lse[rows].double() - score).abs() <= 2.0 ** -20 * abs(score)).all(), (lse[rows].flatten()[:4], score)
+
+
+def equal_keys(q_rows, keys, heads, d, dtype, lead, seed):
+    """Queries against one key over and over, but for one in the first tile that is `lead` further along; V of ones but for that key's. Keys
+    but that one have the same weight in a row: exp(-x), x = lead * scale * sum q."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    Q = torch.rand(q_rows, heads, d, generator=g, device=DEV).to(TYPES[dtype])
+    K = torch.full((keys, heads, d), 0.5, device=DEV, dtype=TYPES[dtype])
+    K[3] = 0.5 + lead
+    V = torch.ones(keys, heads, d, device=DEV, dtype=TYPES[dtype])
+    scale = d ** -0.5
+    total = Q.double().sum(-1)
+    low, high = total * 0.5 * scale, total * float(K[3, 0, 0]) * scale
+    return Q, K, V, scale, low, high
+
+
+@pytest.mark.parametrize("q_rows,keys,heads,lead", [(32768, 32768, 8, 0.0625), (131072, 131072, 8, 0.0625), (131072, 131072, 8, 0.25), (8192, 131072, 8, 0.0625), (1, 131072, 16, 0.0625)])
+def test_many_equal_keys(q_rows, keys, heads, lead):
+    """Sums of up to 2^17 equal numbers, which all round the same way. lse within what the scores' rounding costs, as in the other tests."""
+    d = 32
+    print(q_rows, keys, heads, lead, flush=True)
+    Q, K, V, scale, low, high = equal_keys(q_rows, keys, heads, d, "f16", lead, 7)
+    if q_rows == keys:
+        assert M.load().maxsim_attention_workspace(1, q_rows, keys, heads, heads, d) == 0  # (in one piece)
+    O, lse = M.maxsim_attention(Q, K, V, R.offsets([q_rows], DEV), R.offsets([keys], DEV), causal=False)
+    torch.cuda.synchronize()
+    want = high + torch.log1p((keys - 1) * torch.exp(low - high))
+    score = (Q.double().abs().sum(-1) * float(K.abs().max())) * scale * 2.0 ** -22 + 2.0 ** -20
+    off = (lse.double() - want).abs() / (score + 2.0 ** -22 * want.abs())
+    print("lse: %.3g of the bound" % float(off.max()), flush=True)
+    u = R.UNIT[Q.dtype]
+    off_o = (O.double() - 1).abs() / (u + score + 2e-6 + u)[..., None]
+    print("O: %.3g of the bound" % float(off_o.max()), flush=True)
+    assert off.max() <= 1 and off_o.max() <= 1
