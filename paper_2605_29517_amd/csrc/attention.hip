@@ -3,8 +3,8 @@
 // One pass over the keys with a running maximum and sum (in 32 bits): a workgroup owns ROWS rows (a row: one token of one query
 // head; the heads that share keys lie side by side, so that a token's whole group reads K and V once), a wavefront 32 of them, and
 // walks the keys in tiles of 64 (32 at d = 256) that are copied to LDS one tile ahead. P is rounded to the inputs' 16-bit type for the second
-// product (relative error 2^-9 in bf16, 2^-12 in fp16, no more than the rounding of the output; the sum that divides it
-// stays in 32 bits).
+// product (relative error at most 2^-8 in bf16, 2^-11 in fp16 and the 2^-32 of the largest weight that stand at LIFT: no more than the rounding of the
+// output, of any size up to 2^21 keys; the sum that divides it stays in 32 bits).
 #include "attention.h"
 
 #include <cmath>
@@ -13,7 +13,11 @@ namespace maxsim {
 namespace {
 
 constexpr float NO_MAXIMUM = -3.4028234664e38f; // of a row that has seen no key, the lowest finite number, so that no difference of infinities arises
-constexpr float LAZY = 8.0f;            // the maximum may lag by this many powers of two: P <= 2^8, far from overflow in fp16
+constexpr float LAZY = 8.0f;                    // the maximum may lag by this many powers of two
+// fp16 has no normal numbers below 2^-14 and none below 2^-24, while the sum in 32 bits counts every weight: P are taken 2^7 times as large, which with
+// LAZY is at most 2^15. Then a weight is off by its rounding and by 2^-32 of the largest at most (2^-25 without): of one key and 10^5 others of 2^-26 of its
+// weight 10^-5 of the result is lost instead of all that the others make, 10^-3.
+template <int DT> constexpr float LIFT = DT == MAXSIM_F16 ? 7.0f : 0.0f;
 // P = exp2(scale_log2 S - scale_log2 top) by one fma, with top among the scores S as they are. The fma's product is exact and the number that it
 // subtracts is rounded, so that all of a row's P are off by one factor, which the sum that divides them shares: 2^-4 of an exponent at
 // FAR, but more than P can hold from 2^28 on. Further out than FAR the difference is taken first: scores of +-10^38 (bf16) are told apart as fp32 tells them.
@@ -53,7 +57,10 @@ __device__ __forceinline__ float attn_tree(const f32x16 &x)
 }
 
 // Of a row that sees keys
-__device__ __forceinline__ float attn_lse(const AttnParams &p, float top, float sum) { return __builtin_fmaf(top, p.scale, __builtin_amdgcn_logf(sum) * 0.69314718055994531f); }
+template <int DT> __device__ __forceinline__ float attn_lse(const AttnParams &p, float top, float sum)
+{
+    return __builtin_fmaf(top, p.scale, (__builtin_amdgcn_logf(sum) - LIFT<DT>) * 0.69314718055994531f);
+}
 
 // A column's result: O = o / sum and lse, or the same of a piece. `seen`: that there is a key, which the mask says and not the sum, so that a sum which
 // is not a number shows in lse (with NaNs not honoured by the compiler a comparison of it would say anything).
@@ -189,9 +196,9 @@ template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, DP 
                 for (int r = 0; r < 16; ++r)
                     o[b][r] *= by;
         }
-        float less = top * p.scale_log2;
+        float less = __builtin_fmaf(top, p.scale_log2, -LIFT<DT>);
         if (__builtin_amdgcn_ballot_w64(fabsf(less) > FAR)) {
-            less = 0.0f;
+            less = -LIFT<DT>;
 #pragma unroll
             for (int b = 0; b < B; ++b)
 #pragma unroll
@@ -238,7 +245,7 @@ template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, DP 
     const float sum = attn_halves_sum(sums.sum - sums.lost);
     if (p.n_split > 1) {
         if (row < rows)
-            attn_write<DT>(p, o, attn_lse(p, top, sum), sum, limit > t0 * TILE, piece, q.start + token, head, h);
+            attn_write<DT>(p, o, attn_lse<DT>(p, top, sum), sum, limit > t0 * TILE, piece, q.start + token, head, h);
         return;
     }
     __syncthreads(); // (nobody reads the tiles any more)
@@ -249,7 +256,7 @@ template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, DP 
         return p.O.p + (uint64_t)t * p.O.token + (hk * p.pack + g) * p.O.head;
     });
     if (p.lse && h == 0 && row < rows)
-        p.lse[(q.start + token) * p.hq + head] = seen ? attn_lse(p, top, sum) : neg_inf();
+        p.lse[(q.start + token) * p.hq + head] = seen ? attn_lse<DT>(p, top, sum) : neg_inf();
 }
 
 // The same for few rows per sequence (single tokens against kept keys): what counts is that keys and values stream at the memory's
@@ -355,9 +362,9 @@ template <int DT, int DP> __global__ void __launch_bounds__(NF * 64, 1) attn_few
                 for (int r = 0; r < 16; ++r)
                     o[b][r] *= by;
         }
-        float less = top * p.scale_log2;
+        float less = __builtin_fmaf(top, p.scale_log2, -LIFT<DT>);
         if (__builtin_amdgcn_ballot_w64(fabsf(less) > FAR)) {
-            less = 0.0f;
+            less = -LIFT<DT>;
 #pragma unroll
             for (int r = 0; r < 16; ++r)
                 s[r] -= top;
@@ -415,7 +422,7 @@ template <int DT, int DP> __global__ void __launch_bounds__(NF * 64, 1) attn_few
                 o[b][r] = o[b][r] * by + theirs[(b * 16 + r) * 64] * by2;
     }
     if (row < rows)
-        attn_write<DT>(p, o, attn_lse(p, top, sum), sum, limit > start * KEYS, piece, q.start + token, head, h);
+        attn_write<DT>(p, o, attn_lse<DT>(p, top, sum), sum, limit > start * KEYS, piece, q.start + token, head, h);
 }
 
 // Joins the pieces of a row: weights exp(lse_piece - lse). Eight lanes read 128 bytes of a piece; PIECES such groups, 1 or the 8 of a wavefront,

@@ -138,3 +138,30 @@ def test_many_equal_keys(q_rows, keys, heads, lead):
     off_o = (O.double() - 1).abs() / (u + score + 2e-6 + u)[..., None]
     print("O: %.3g of the bound" % float(off_o.max()), flush=True)
     assert off.max() <= 1 and off_o.max() <= 1
+
+
+@pytest.mark.parametrize("q_rows,keys,heads", [(100_000, 100_000, 8), (8192, 100_000, 8), (1, 100_000, 16), (1, 300_000, 16)])
+def test_many_small_weights(q_rows, keys, heads):
+    """One key ahead of 10^5 others by about 2^26: these make 10^-3 of the result, of weights that fp16 has no normal numbers for. A weight may be off by its
+    rounding and by 2^-32 of the largest."""
+    d = 32
+    print(q_rows, keys, heads, flush=True)
+    Q = torch.full((q_rows, heads, d), 1.0, device=DEV, dtype=torch.float16)
+    Q += torch.arange(q_rows, device=DEV)[:, None, None] % 7 * 2.0 ** -6
+    K = torch.zeros(keys, heads, d, device=DEV, dtype=torch.float16)
+    scale = d ** -0.5
+    K[5] = 3.25
+    V = torch.ones(keys, heads, d, device=DEV, dtype=torch.float16)
+    V[5] = 0
+    O, lse = M.maxsim_attention(Q, K, V, R.offsets([q_rows], DEV), R.offsets([keys], DEV), causal=False, scale=scale)
+    torch.cuda.synchronize()
+    x = Q.double().sum(-1) * 3.25 * scale
+    p = torch.exp(-x) / (1 + (keys - 1) * torch.exp(-x))
+    want = (keys - 1) * p
+    print("weights 2^%.1f .. 2^%.1f" % (float(torch.log2(p.min())), float(torch.log2(p.max()))), flush=True)
+    u, score = R.UNIT[Q.dtype], x * 2.0 ** -22 + 2.0 ** -20
+    err = want * (u + score + 2e-6) + (keys - 1) * 2.0 ** -32
+    bound = err + u * (want + err) + R.TINY[Q.dtype]
+    off = ((O.double() - want[..., None]).abs() / bound[..., None]).max()
+    print("%.3g of the bound" % float(off), flush=True)
+    assert off <= 1
