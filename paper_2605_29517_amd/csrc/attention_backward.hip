@@ -22,7 +22,10 @@ constexpr int Q_TILE = 32; // query rows per step of the dK, dV kernel
 //   dK    takes delta plus the sum of dS over the row's keys, which is what delta was short of (it is zero for the right one);
 //   dQ    of rows of up to EXACT_KEYS keys: delta is summed from P dP in a pass of its own, which needs no O;
 //   dQ    of more keys: dS is rounded in two parts, so that delta's part is nearly all that is left; one product more, beside the same operand.
-// Under a causal mask rows of more than SPLIT_KEYS_CAUSAL keys bring little of the gradient, and stay as they are. What the last two cost: 500 texts
+// Under a causal mask rows of more than SPLIT_KEYS_CAUSAL keys bring little of the gradient beside the first rows, and stay as they are; not so where
+// keys are kept before the first row, which all see many then (256 rows of heads of 64 after 600 kept keys: 1.60 times without the
+// second part, 1.23 with it; the gradient of eight times 256 rows after 1244 to 3744 keys, 16 heads of 128 over 4, takes 235 us for 214).
+// What the last two cost: 500 texts
 // of 100 tokens, 16 heads of 128 over 4, 379 us of gradient without, 396 with; 64 x 1024 tokens of 12 heads of 64, no mask, 745 and 826.
 constexpr int EXACT_KEYS = 128, SPLIT_KEYS_CAUSAL = 512;
 constexpr float LOG2E = 1.44269504088896341f;
@@ -62,7 +65,7 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, DP > 128 ? 
     const AttnRowRead<DP> row_read(lane);
     const AttnColRead<DP> col_read(lane);
     const int tiles = (wg_keys + TILE - 1) / TILE;
-    const bool exact = wg_keys <= EXACT_KEYS, twice = !exact && (!p.causal || wg_keys <= SPLIT_KEYS_CAUSAL);
+    const bool exact = wg_keys <= EXACT_KEYS, twice = !exact && (!p.causal || wg_keys <= SPLIT_KEYS_CAUSAL || ahead > 0);
     auto issue = [&](int buffer, int t) {
         const uint32_t to = attn_lds(lds) + buffer * 2 * TILE_BYTES;
         copy.issue(k_head, p.K.token, t * TILE, k.len - 1, to, w, p.d);

@@ -165,3 +165,20 @@ def test_many_small_weights(q_rows, keys, heads):
     off = ((O.double() - want[..., None]).abs() / bound[..., None]).max()
     print("%.3g of the bound" % float(off), flush=True)
     assert off <= 1
+
+
+@pytest.mark.parametrize("n,kept", [(256, 0), (256, 200), (256, 450), (256, 600), (256, 4000), (1500, 300)])
+@pytest.mark.parametrize("d,dtype", [(64, "bf16"), (64, "f16"), (128, "bf16"), (128, "f16")])
+def test_errors_in_the_norm_after_kept_keys(n, kept, d, dtype):
+    """Causal queries after keys that are kept: rows that see many keys, all of them. The bound of the same test without kept keys."""
+    Q, K, V, dO, qo, ko = inputs([n] * 2, [n + kept] * 2, 8, 2, d, dtype)
+    O, lse = M.maxsim_attention(Q, K, V, qo, ko)
+    grads = M.maxsim_attention_backward(Q, K, V, O, lse, dO, qo, ko)
+    torch.cuda.synchronize()
+    want = R.attention(Q, K, V, qo, ko, True, d ** -0.5, dO)
+    for name, x in zip(("O", "dQ", "dK", "dV"), (O, *grads)):
+        value = want[name][0]
+        alone = (value.to(Q.dtype).double() - value).norm()
+        off = (x.double() - value).norm()
+        print(n, kept, d, dtype, name, "%.3f" % float(off / alone), flush=True)
+        assert off <= 1.5 * alone, name
