@@ -12,9 +12,10 @@ def rope_frequencies(rot, base=10000.0, factor=1.0, scaling=None, original=4096,
       None     as trained
       "linear" positions are interpolated: every angle is divided by factor
       "base"   the base grows by factor^(rot / (rot - 2)): the slowest pair is interpolated by factor, the fastest one stays
-      "parts"  by wavelength: pairs that turn at least `fast` times within the original length stay, those that turn at most `slow`
-               times are interpolated, between them the angle goes over linearly (in the pair's number); cosines and sines are scaled by
-               0.1 ln(factor) + 1, which sharpens the softmax of the longer rows
+      "parts"  by wavelength, the method of "YaRN: Efficient Context Window Extension of Large Language Models" (Peng et al., 2023): pairs that turn
+               at least `fast` times within the original length stay, those that turn at most `slow` times are interpolated, between them the
+               angle goes over linearly (in the pair's number); cosines and sines are scaled by 0.1 ln(factor) + 1, which sharpens the softmax
+               of the longer rows
     """
     if rot < 2 or rot % 2:
         raise ValueError("rot must be even and at least 2")
@@ -36,7 +37,8 @@ def rope_frequencies(rot, base=10000.0, factor=1.0, scaling=None, original=4096,
         def number(turns):  # of the pair that turns so many times within the original length
             return rot * math.log(original / (turns * 2 * math.pi)) / (2 * math.log(base))
 
-        first, last = max(math.floor(number(fast)), 0), min(math.ceil(number(slow)), rot // 2 - 1)
+        # (the end may lie past the last pair, which then is not interpolated in full; the bounds 0 and rot - 1 are the published ones)
+        first, last = max(math.floor(number(fast)), 0), min(math.ceil(number(slow)), rot - 1)
         share = ((pair / 2 - first) / max(last - first, 1e-3)).clamp(0.0, 1.0)  # of the interpolated angle
         freqs = freqs * (1.0 - share) + freqs / factor * share
         scale = 0.1 * math.log(factor) + 1.0
