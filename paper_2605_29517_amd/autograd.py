@@ -1,9 +1,19 @@
 """torch.autograd glue over the C ABI (marshalling only): the forward keeps the int32 argmax the kernels
 emit (Sec. "Closed-Form Gradients"), the backward hands it with the upstream gradient to maxsim_backward.
-Nothing is computed here; every step runs in the HIP kernels, and there is no CPU fallback."""
+Nothing is computed here; every step runs in the HIP kernels, and there is no CPU fallback.
+
+Scores and attention can be differentiated once: to go on through a gradient that was made with create_graph=True raises an error (the
+kernels leave no graph of it). Rotary positions are linear and can be differentiated any number of times."""
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as M
+
+
+def _once(backward):
+    """once_differentiable where a graph of the gradient is asked for; elsewhere backward as it is (a microsecond of a small step)."""
+    guarded = once_differentiable(backward)
+    return lambda ctx, g: guarded(ctx, g) if torch.is_grad_enabled() else backward(ctx, g)
 
 
 class _MaxSim(torch.autograd.Function):
@@ -14,6 +24,7 @@ class _MaxSim(torch.autograd.Function):
         return scores
 
     @staticmethod
+    @_once
     def backward(ctx, dscore):
         Q, D, argmax = ctx.saved_tensors
         dQ, dD = M.maxsim_backward(Q, D, argmax, dscore.contiguous().float())
@@ -28,6 +39,7 @@ class _MaxSimRagged(torch.autograd.Function):
         return scores
 
     @staticmethod
+    @_once
     def backward(ctx, dscore):
         Q, D_packed, doc_offsets, argmax = ctx.saved_tensors
         dQ, dD = M.maxsim_backward_ragged(Q, D_packed, doc_offsets, argmax, dscore.contiguous().float())
@@ -51,16 +63,16 @@ def _rows(t):
 
 class _Rope(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, X, freqs, positions, offsets, interleaved, scale):
+    def forward(ctx, X, freqs, positions, offsets, interleaved, scale, inverse):
         ctx.save_for_backward(freqs, positions, offsets)
-        ctx.how = interleaved, scale
-        return M.maxsim_rope(_rows(X), freqs, positions, offsets, interleaved=interleaved, scale=scale)
+        ctx.how = interleaved, scale, inverse
+        return M.maxsim_rope(_rows(X), freqs, positions, offsets, interleaved=interleaved, scale=scale, inverse=inverse)
 
     @staticmethod
     def backward(ctx, dY):
         freqs, positions, offsets = ctx.saved_tensors
-        interleaved, scale = ctx.how
-        return M.maxsim_rope(_rows(dY), freqs, positions, offsets, interleaved=interleaved, scale=scale, inverse=True), None, None, None, None, None
+        interleaved, scale, inverse = ctx.how
+        return (_Rope.apply(dY, freqs, positions, offsets, interleaved, scale, not inverse),) + (None,) * 6
 
 
 class _Attention(torch.autograd.Function):
@@ -73,6 +85,7 @@ class _Attention(torch.autograd.Function):
         return out
 
     @staticmethod
+    @_once
     def backward(ctx, dout):
         Q, K, V, out, lse, q_offsets, k_offsets = ctx.saved_tensors
         causal, scale = ctx.how
@@ -81,7 +94,7 @@ class _Attention(torch.autograd.Function):
 
 def rope(X, freqs, positions=None, offsets=None, interleaved=False, scale=1.0):
     """Differentiable rotary positions of X [tokens, heads, d] (binding.maxsim_rope; no gradient for freqs)."""
-    return _Rope.apply(X, freqs, positions, offsets, interleaved, scale)
+    return _Rope.apply(X, freqs, positions, offsets, interleaved, scale, False)
 
 
 def attention(Q, K, V, q_offsets, k_offsets=None, causal=True, scale=None):
