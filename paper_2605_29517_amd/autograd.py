@@ -55,10 +55,17 @@ def maxsim(Q, D, doc_offsets=None):
 
 
 def _rows(t):
-    """t as the attention and rotary entry points take it: rows of stride 1 in pieces of 16 bytes (a view if it is one of those)."""
+    """t as the rotary entry point takes it fastest: rows of stride 1 in pieces of 16 bytes (a view if it is one of those)."""
     size = t.element_size()
     fine = t.dim() == 3 and t.stride(2) == 1 and (t.data_ptr() | t.stride(0) * size | t.stride(1) * size) % 16 == 0
     return t if fine else t.contiguous()
+
+
+def _pieces(t):
+    """t as the attention entry points take it: rows of stride 1 in pieces of 16 bytes, less than 2^24 entries apart (a view if it is one of
+    those, otherwise a copy, also where t is contiguous but at an odd address)."""
+    t = _rows(t)
+    return t if t.data_ptr() % 16 == 0 and t.stride(0) < 1 << 24 else t.clone(memory_format=torch.contiguous_format)
 
 
 class _Rope(torch.autograd.Function):
@@ -78,7 +85,7 @@ class _Rope(torch.autograd.Function):
 class _Attention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, Q, K, V, q_offsets, k_offsets, causal, scale):
-        Q, K, V = _rows(Q), _rows(K), _rows(V)
+        Q, K, V = _pieces(Q), _pieces(K), _pieces(V)
         out, lse = M.maxsim_attention(Q, K, V, q_offsets, k_offsets, causal=causal, scale=scale)
         ctx.save_for_backward(Q, K, V, out, lse, q_offsets, k_offsets)
         ctx.how = causal, scale
@@ -89,7 +96,7 @@ class _Attention(torch.autograd.Function):
     def backward(ctx, dout):
         Q, K, V, out, lse, q_offsets, k_offsets = ctx.saved_tensors
         causal, scale = ctx.how
-        return M.maxsim_attention_backward(Q, K, V, out, lse, _rows(dout), q_offsets, k_offsets, causal=causal, scale=scale) + (None,) * 4
+        return M.maxsim_attention_backward(Q, K, V, out, lse, _pieces(dout), q_offsets, k_offsets, causal=causal, scale=scale) + (None,) * 4
 
 
 def rope(X, freqs, positions=None, offsets=None, interleaved=False, scale=1.0):

@@ -82,3 +82,53 @@ def test_attention_and_maxsim_refuse_second_derivatives(plain):
     grads = torch.autograd.grad(A.maxsim(Q, D).square().sum(), (Q, D), create_graph=True)
     with pytest.raises(RuntimeError, match="once_differentiable"):
         (Q.sum() + grads[1].square().sum()).backward()
+
+
+def acceptable(t):
+    """What the C side asks of a tensor's address and strides (in elements of 16 bits)."""
+    token, head = t.stride(0) if t.shape[0] > 1 else t.shape[2], t.stride(1) if t.shape[1] > 1 else t.shape[2]
+    return t.stride(2) == 1 and t.data_ptr() % 16 == 0 and token % 8 == 0 and head % 8 == 0 and token < 1 << 24
+
+
+def odd(shape, by):
+    """A contiguous view at an address that is no multiple of 16 bytes."""
+    flat = torch.randn(torch.Size(shape).numel() + by, generator=torch.Generator().manual_seed(5)).half()
+    return flat[by:].view(shape)
+
+
+LAYOUTS = {
+    "odd address": lambda: odd((6, 2, 8), 1),
+    "slice of odd rows": lambda: odd((6, 2, 12), 0)[:, :, :8],
+    "innermost not 1": lambda: odd((6, 8, 2), 0).transpose(1, 2),
+    "expanded": lambda: odd((1, 1, 1), 0).expand(6, 2, 8),
+    "rows too far apart": lambda: torch.zeros(5 * (1 << 24) + 16, dtype=torch.float16).as_strided((6, 2, 8), (1 << 24, 8, 1)),
+    "fitting view": lambda: odd((6, 4, 8), 0)[:, 1:3],
+}
+
+
+@pytest.mark.parametrize("layout", LAYOUTS)
+def test_attention_of_any_layout(monkeypatch, layout):
+    """Inputs and upstream gradients that the kernels do not take as they lie are copied; what they do take is not."""
+    seen = []
+
+    class Entry(Plain):
+        @staticmethod
+        def maxsim_attention(Q, K, V, *a, **k):
+            seen.extend((Q, K, V))
+            return torch.zeros(Q.shape, dtype=Q.dtype), torch.zeros(Q.shape[:2])
+
+        @staticmethod
+        def maxsim_attention_backward(Q, K, V, out, lse, dout, *a, **k):
+            seen.append(dout)
+            return torch.zeros(Q.shape).half(), torch.zeros(K.shape).half(), torch.zeros(V.shape).half()
+
+    monkeypatch.setattr(A, "M", Entry)
+    t = LAYOUTS[layout]()
+    leaf = t.detach().clone().requires_grad_()
+    out = A.attention(t, t, leaf, torch.tensor([0, 6], dtype=torch.int32))
+    out.backward(LAYOUTS[layout]())
+    assert len(seen) == 4
+    for x in seen:
+        assert acceptable(x) and torch.equal(x, t), (layout, x.stride(), x.data_ptr() % 16)
+    if layout == "fitting view":
+        assert seen[0] is t or seen[0].data_ptr() == t.data_ptr()
