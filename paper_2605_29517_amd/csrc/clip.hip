@@ -89,7 +89,7 @@ template <bool ONCE, class T> __device__ __forceinline__ double chunk_squares(co
     }
     return sum;
 }
-template <bool ONCE, class T> __device__ __forceinline__ void chunk_scaled(const T *g, T *out, int n, float by)
+template <bool ONCE, class T> __device__ __forceinline__ void chunk_scaled(const T *g, T *out, int n, float by, float more)
 {
     constexpr int V = Vec<T>::V, STEPS = CHUNK / (WG * V);
     if (n == CHUNK) {
@@ -101,12 +101,12 @@ template <bool ONCE, class T> __device__ __forceinline__ void chunk_scaled(const
         for (int s = 0; s < STEPS; ++s) {
 #pragma unroll
             for (int i = 0; i < V; ++i)
-                x[s].x[i] = (T)((float)x[s].x[i] * by);
+                x[s].x[i] = (T)((float)x[s].x[i] * by * more);
             store_vec<ONCE>(out + (s * WG + threadIdx.x) * V, x[s]);
         }
     } else {
         for (int e = threadIdx.x; e < n; e += WG)
-            out[e] = (T)((float)g[e] * by);
+            out[e] = (T)((float)g[e] * by * more);
     }
 }
 
@@ -171,11 +171,13 @@ template <bool ONCE, class Tensors> __global__ void __launch_bounds__(WG) clip_s
     double sum = 0.0;
     for (int x = threadIdx.x; x < parts; x += WG)
         sum += part[x];
-    const float total = (float)sqrt(wg_sum(sum));
+    const double total = sqrt(wg_sum(sum));
     if (blockIdx.x == 0 && threadIdx.x == 0)
-        *norm = total;
-    const float by0 = max_norm / (total + 1e-6f);
-    const float by = by0 < 1.0f || by0 != by0 ? by0 : 1.0f;
+        *norm = (float)total;
+    // The factor in 64 bits, since the norm of fp32 numbers need not be one; one that fp32 holds badly or not at all as a product of two
+    const double by0 = (double)max_norm / (total + 1e-6);
+    const bool small = by0 < 0x1p-100;
+    const float by = small ? 0x1p-100f : (float)(by0 < 1.0 || by0 != by0 ? by0 : 1.0), more = small ? (float)(by0 * 0x1p100) : 1.0f;
     const int64_t c0 = chunks * blockIdx.x / gridDim.x, c1 = chunks * (blockIdx.x + 1) / gridDim.x;
     if (c0 >= c1)
         return;
@@ -188,11 +190,11 @@ template <bool ONCE, class Tensors> __global__ void __launch_bounds__(WG) clip_s
         const int64_t e = (c - t.chunk[i]) * CHUNK, left = t.numel[i] - e;
         const int m = left < CHUNK ? (int)left : CHUNK;
         if (t.dtype[i] == MAXSIM_F32)
-            chunk_scaled<ONCE>(static_cast<const float *>(t.g[i]) + e, static_cast<float *>(t.out[i]) + e, m, by);
+            chunk_scaled<ONCE>(static_cast<const float *>(t.g[i]) + e, static_cast<float *>(t.out[i]) + e, m, by, more);
         else if (t.dtype[i] == MAXSIM_F16)
-            chunk_scaled<ONCE>(static_cast<const _Float16 *>(t.g[i]) + e, static_cast<_Float16 *>(t.out[i]) + e, m, by);
+            chunk_scaled<ONCE>(static_cast<const _Float16 *>(t.g[i]) + e, static_cast<_Float16 *>(t.out[i]) + e, m, by, more);
         else
-            chunk_scaled<ONCE>(static_cast<const __bf16 *>(t.g[i]) + e, static_cast<__bf16 *>(t.out[i]) + e, m, by);
+            chunk_scaled<ONCE>(static_cast<const __bf16 *>(t.g[i]) + e, static_cast<__bf16 *>(t.out[i]) + e, m, by, more);
     }
 }
 
