@@ -259,7 +259,8 @@ int maxsim_ce_grad(const float *scores, int n, int b, float tau, float *g, float
  * of maxsim_forward_ragged is: token rows back to back, with int32 offsets on the device.
  *
  * Packed tensors [tokens, heads, d] of these entry points may be views (slices of a fused projection, transposed
- * heads): strides are counted in elements, the innermost one is 1.
+ * heads): strides are counted in elements, the innermost one is 1.  Rows of an output lie apart: a token's heads
+ * before the next token or a head's tokens before the next head; other strides are refused.
  */
 
 /*
@@ -267,7 +268,7 @@ int maxsim_ce_grad(const float *scores, int n, int b, float tau, float *g, float
  *     y_i = scale (x_i cos a - x_j sin a),  y_j = scale (x_i sin a + x_j cos a),  a = p(t) * freqs[i],
  * with j = i + rot / 2 or, with `neighbours`, the pair (2 i, 2 i + 1).  Entries from rot on are copied.  With
  * `inverse` the angle's sign is turned: the transposed map, hence the gradient of the forward one.
- *   X, Y       [tokens, heads, d] dtype    Y may be X (and is otherwise apart from it)
+ *   X, Y       [tokens, heads, d] dtype    Y may be X, with X's strides (and is otherwise apart from it)
  *   freqs      [rot / 2] float32           angle per position; 2 <= rot <= d, even, rot <= 4096
  *   positions  [tokens] int32 or NULL      p(t); NULL: the place of t in its sequence
  *   offsets    [b + 1] int32 or NULL       the sequences (not looked at where positions are given); NULL: one sequence

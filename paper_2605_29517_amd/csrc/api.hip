@@ -142,6 +142,14 @@ hipStream_t copy_stream()
     return cached[dev];
 }
 
+// Whether the rows of an output [tokens, heads, d] lie apart: a token's heads before the next token, or a head's tokens before the next head (strides >= 0)
+bool rows_apart(int64_t tokens, int64_t heads, int64_t d, int64_t token, int64_t head)
+{
+    if (token < d || head < d)
+        return false;
+    return tokens == 1 || heads == 1 || token >= __int128(heads - 1) * head + d || head >= __int128(tokens - 1) * token + d;
+}
+
 // Attention: sizes, then pointers and strides of the packed tensors
 int attention_sizes_ok(int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, int hkv, int d)
 {
@@ -160,7 +168,7 @@ struct AttnTensor {
     maxsim::AttnRows *to;
     const void *p;
     int heads;
-    bool written;
+    int64_t rows; // of an output, 0 otherwise
 };
 
 int attention_common(maxsim::AttnParams &p, const AttnTensor *t, int n, const int64_t *strides, const int32_t *q_offsets, const int32_t *k_offsets, int64_t b, int64_t q_tokens,
@@ -176,7 +184,7 @@ int attention_common(maxsim::AttnParams &p, const AttnTensor *t, int n, const in
         const int64_t token = strides ? strides[2 * i] : (int64_t)t[i].heads * d, head = strides ? strides[2 * i + 1] : d;
         if (!t[i].p || !aligned(t[i].p, 16) || token < 0 || head < 0 || token % 8 != 0 || head % 8 != 0)
             return MAXSIM_ERR_INVALID;
-        if (t[i].written && (token < d || head < d)) // rows of an output lie apart
+        if (t[i].rows && !rows_apart(t[i].rows, t[i].heads, d, token, head))
             return MAXSIM_ERR_INVALID;
         if (token >= (1 << 24) || head >= (int64_t(1) << 40))
             return MAXSIM_ERR_UNSUPPORTED;
@@ -573,7 +581,7 @@ int maxsim_rope(const void *X, int64_t tokens, int heads, int d, int64_t x_token
 {
     if (!X || !Y || !freqs || tokens < 1 || heads < 1 || d < 2 || rot < 2 || rot > d || rot % 2 != 0 || !dtype_ok((int)dtype) || (offsets && b < 1) || is_nan(scale))
         return MAXSIM_ERR_INVALID;
-    if (x_token_stride < 0 || x_head_stride < 0 || y_token_stride < d || y_head_stride < d) // rows of an output lie apart
+    if (x_token_stride < 0 || x_head_stride < 0 || !rows_apart(tokens, heads, d, y_token_stride, y_head_stride))
         return MAXSIM_ERR_INVALID;
     const uintptr_t size = dtype == MAXSIM_F32 ? 4 : 2;
     if (!aligned(X, size) || !aligned(Y, size) || !aligned(freqs, 4) || !aligned(positions, 4) || !aligned(offsets, 4))
@@ -596,7 +604,7 @@ int maxsim_attention(const void *Q, const void *K, const void *V, const int64_t 
                      void *stream)
 {
     maxsim::AttnParams p = {};
-    const AttnTensor t[4] = {{&p.Q, Q, hq}, {&p.K, K, hkv}, {&p.V, V, hkv}, {&p.O, O, hq, true}};
+    const AttnTensor t[4] = {{&p.Q, Q, hq}, {&p.K, K, hkv}, {&p.V, V, hkv}, {&p.O, O, hq, q_tokens}};
     if (int rc = attention_common(p, t, 4, strides, q_offsets, k_offsets, b, q_tokens, k_tokens, hq, hkv, d, dtype, causal, scale, workspace, workspace_bytes,
                                   maxsim_attention_workspace(b, q_tokens, k_tokens, hq, hkv, d)))
         return rc;
@@ -618,7 +626,7 @@ int maxsim_attention_backward(const void *Q, const void *K, const void *V, const
                               void *dQ, void *dK, void *dV, void *workspace, int64_t workspace_bytes, void *stream)
 {
     maxsim::AttnParams p = {};
-    const AttnTensor t[8] = {{&p.Q, Q, hq}, {&p.K, K, hkv}, {&p.V, V, hkv}, {&p.O, O, hq}, {&p.dO, dO, hq}, {&p.dQ, dQ, hq, true}, {&p.dK, dK, hkv, true}, {&p.dV, dV, hkv, true}};
+    const AttnTensor t[8] = {{&p.Q, Q, hq}, {&p.K, K, hkv}, {&p.V, V, hkv}, {&p.O, O, hq}, {&p.dO, dO, hq}, {&p.dQ, dQ, hq, q_tokens}, {&p.dK, dK, hkv, k_tokens}, {&p.dV, dV, hkv, k_tokens}};
     if (int rc = attention_common(p, t, 8, strides, q_offsets, k_offsets, b, q_tokens, k_tokens, hq, hkv, d, dtype, causal, scale, workspace, workspace_bytes,
                                   maxsim_attention_backward_workspace(b, q_tokens, k_tokens, hq, hkv, d)))
         return rc;
