@@ -182,3 +182,60 @@ def test_errors_in_the_norm_after_kept_keys(n, kept, d, dtype):
         off = (x.double() - value).norm()
         print(n, kept, d, dtype, name, "%.3f" % float(off / alone), flush=True)
         assert off <= 1.5 * alone, name
+
+
+@pytest.mark.parametrize("name,q,k,hq,hkv,d,dtype", [
+    ("streamed", [1, 1, 1], [24000, 700, 9000], 32, 8, 128, "bf16"),
+    ("streamed, heads of 72", [2, 1], [30000, 17000], 16, 8, 72, "f16"),
+    ("pieces", [1, 2], [20011, 3000], 8, 2, 128, "bf16"),
+    ("pieces of many rows", [100, 30], [8192, 4097], 4, 2, 64, "f16"),
+])
+def test_views_of_a_cache(name, q, k, hq, hkv, d, dtype):
+    """Keys and values as slices of one tensor and with heads before tokens, a result into a slice: the same bits as without gaps, in one piece and joined."""
+    print(name, flush=True)
+    Q, K, V, _, qo, ko = inputs(q, k, hq, hkv, d, dtype)
+    if name.startswith("streamed"):
+        assert sum(k) * hkv * d * 4 >= 1e8
+    else:
+        assert M.load().maxsim_attention_workspace(len(q), sum(q), sum(k), hq, hkv, d) > 0
+    want = M.maxsim_attention(Q, K, V, qo, ko)
+    both = torch.cat((K, V), 1)
+    turned = [t.transpose(0, 1).contiguous().transpose(0, 1) for t in (K, V)]
+    room = torch.full((sum(q), 3 * hq, d), float("nan"), device=DEV, dtype=Q.dtype)
+    for a, b in ((both[:, :hkv], both[:, hkv:]), turned, (both[:, :hkv], turned[1])):
+        O, lse = M.maxsim_attention(Q.transpose(0, 1).contiguous().transpose(0, 1), a, b, qo, ko, out=room[:, hq:2 * hq])
+        torch.cuda.synchronize()
+        assert torch.equal(O, want[0]) and torch.equal(lse, want[1])
+        assert room[:, :hq].isnan().all() and room[:, 2 * hq:].isnan().all()
+        room.fill_(float("nan"))
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("q,k,hq,hkv,d,dtype", [([32], [20000], 8, 2, 128, "bf16"), ([1, 7, 40], [9000, 4097, 3000], 4, 1, 64, "f16"), ([5], [6000], 2, 2, 256, "bf16")])
+def test_gradient_of_few_queries_after_many_keys(q, k, hq, hkv, d, dtype, causal):
+    print(q, k, hq, hkv, d, dtype, causal, flush=True)
+    Q, K, V, dO, qo, ko = inputs(q, k, hq, hkv, d, dtype)
+    got = run(Q, K, V, dO, qo, ko, causal)
+    want = R.attention(Q, K, V, qo, ko, causal, d ** -0.5, dO)
+    for name in want:
+        R.check(name, got[name], want[name])
+
+
+def test_autograd_of_odd_addresses():
+    """The differentiable form of inputs, and with an upstream gradient, that lie at no multiple of 16 bytes: as of copies that do."""
+    from paper_2605_29517_amd import autograd as A
+    lens = [33, 70]
+    Q, K, V, dO, qo, _ = inputs(lens, lens, 4, 2, 64, "bf16")
+
+    def odd(t):
+        return torch.cat((t.flatten()[:1], t.flatten()))[1:].view(t.shape)
+
+    results = []
+    for move in (lambda t: t.clone(), odd):
+        leaf = [t.clone().requires_grad_() for t in (Q, K, V)]
+        out = A.attention(*(move(t) if move is odd else t for t in leaf), qo)
+        out.backward(move(dO))
+        results.append([out.detach()] + [t.grad for t in leaf])
+    assert odd(dO).data_ptr() % 16 != 0
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
