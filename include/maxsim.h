@@ -290,7 +290,7 @@ int maxsim_rope(const void *X, int64_t tokens, int heads, int d, int64_t x_token
  *   strides  HOST int64 [8]: token and head stride of Q, K, V, O in this order, multiples of 8 and token strides below
  *         2^24; NULL: all without gaps.  Base pointers are multiples of 16 bytes.
  *   q_offsets, k_offsets [b + 1] int32 (device), as doc_offsets in maxsim_forward_ragged; sequences may be empty
- *   hq    a multiple of hkv;  d  a multiple of 8 up to 256;  scale > 0
+ *   hq    a multiple of hkv;  d  a multiple of 8 up to 256;  10^-30 < scale < 10^30
  *   causal  nonzero: the last query sees all keys, the one before it all but the last, and so on
  *           (query t of lq sees keys j <= t + lk - lq).  Zero: all queries see all keys of their sequence.
  *   lse   [q_tokens, hq] float32 or NULL

@@ -176,7 +176,7 @@ int attention_common(maxsim::AttnParams &p, const AttnTensor *t, int n, const in
 {
     if (int rc = attention_sizes_ok(b, q_tokens, k_tokens, hq, hkv, d))
         return rc;
-    if (!q_offsets || !k_offsets || !aligned(q_offsets, 4) || !aligned(k_offsets, 4) || !dtype_ok(dtype) || is_nan(scale) || scale <= 0.0f || scale >= 1e30f)
+    if (!q_offsets || !k_offsets || !aligned(q_offsets, 4) || !aligned(k_offsets, 4) || !dtype_ok(dtype) || is_nan(scale) || !(scale > 1e-30f && scale < 1e30f)) // (-lse / scale is a finite number)
         return MAXSIM_ERR_INVALID;
     if (dtype == MAXSIM_F32)
         return MAXSIM_ERR_UNSUPPORTED;
