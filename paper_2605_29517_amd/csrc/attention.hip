@@ -21,11 +21,13 @@ template <int DT> constexpr float LIFT = DT == MAXSIM_F16 ? 7.0f : 0.0f;
 // P = exp2(scale_log2 S - scale_log2 top) by one fma, with top among the scores S as they are. The fma's product is exact and the number that it
 // subtracts is rounded, so that all of a row's P are off by one factor, which the sum that divides them shares: 2^-4 of an exponent at
 // FAR, but more than P can hold from 2^28 on. Further out than FAR the difference is taken first: scores of +-10^38 (bf16) are told apart as fp32 tells them.
+// (In the branch that moves the maximum, which such rows take at every step: as a branch of its own, the prompt's kernel copied its scores around it, and
+// 16 sequences of 9 to 130 new tokens took 133 us instead of 120.)
 constexpr float FAR = 1048576.0f;
 
 // The softmax's sum, of which a row has up to millions of terms that may round alike (equal keys): a step's terms are added as a tree, and the steps with
-// what the last addition lost. Added one by one, 2^17 equal keys put lse 226 times as far
-// off as the rounding of the scores may; so it is half of that, for 1 % of the time of short texts (80.6 -> 81.7 us for 250 of them, long prompts 543 -> 545).
+// what the last addition lost. Added one by one, 2^17 equal keys put lse 226 times as far off as the rounding of the scores may; so it is half of
+// that, for 1 to 2 % of the time (250 short texts 71.2 -> 72.2 us, a long prompt 546 -> 547, heads of 256 146 -> 149).
 struct AttnSum {
     float sum, lost; // sum - lost is the value
     __device__ __forceinline__ void add(float x)
@@ -109,16 +111,14 @@ template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, DP 
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // Every XCD takes a contiguous range of (kv head, tile, piece): tiles that read the same keys meet in one L2 (prompt of 8192 tokens
     // 538 us, tile by tile over all heads 955). The last tiles, which see the most keys under a causal mask, come first.
-    const int wg = blockIdx.y * (int)GRID_ROW + blockIdx.x;
-    if (wg >= p.n_wg)
-        return;
+    const int wg = blockIdx.y * (int)GRID_ROW + blockIdx.x; // (those from n_wg on leave below, with the slots that no sequence has: by then the wait for the arguments has passed)
     int v = xcd_grouped(wg, p.n_wg), u = p.by_split(v);
     const int piece = v, hk = p.by_slots(u), slot = p.n_slots - 1 - u;
 
     const AttnPlace place = attn_find_slot<ROWS>(p.q_off, p.b, p.q_tokens, p.pack, slot, p.n_slots);
     const AttnSeq q = place.s, k = p.same ? q : attn_seq(p.k_off, place.i, p.k_tokens);
     const int first = (slot - place.first) * ROWS, rows = q.len * p.pack;
-    if (first < 0 || first >= rows)
+    if (wg >= p.n_wg || first < 0 || first >= rows)
         return;
 
     // this lane's row: the same in both halves
@@ -148,7 +148,8 @@ template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, DP 
 #pragma unroll
         for (int r = 0; r < 16; ++r)
             o[b][r] = 0.0f;
-    float top = NO_MAXIMUM;
+    float top = NO_MAXIMUM, less = 0.0f; // the maximum, and what is subtracted
+    uint64_t far = 0; // rows of the wavefront that are
     AttnSum sums = {0.0f, 0.0f};
 
     const int tiles = (wg_keys + TILE - 1) / TILE;
@@ -186,24 +187,25 @@ template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, DP 
                 m = fmaxf(m, s[b][r]);
         m = attn_halves_max(m);
         // A maximum that grows by less than 2^LAZY is left where it is (the result is the same whatever number is subtracted)
-        if (__builtin_amdgcn_ballot_w64((m - top) * p.scale_log2 > LAZY)) {
+        if (far | __builtin_amdgcn_ballot_w64((m - top) * p.scale_log2 > LAZY)) {
             const float to = fmaxf(m, top), by = __builtin_amdgcn_exp2f((top - to) * p.scale_log2);
             top = to;
+            less = __builtin_fmaf(top, p.scale_log2, -LIFT<DT>);
             sums.scale(by);
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     o[b][r] *= by;
-        }
-        float less = __builtin_fmaf(top, p.scale_log2, -LIFT<DT>);
-        if (__builtin_amdgcn_ballot_w64(fabsf(less) > FAR)) {
-            less = -LIFT<DT>;
+            far = __builtin_amdgcn_ballot_w64(fabsf(less) > FAR);
+            if (far) {
+                less = -LIFT<DT>;
 #pragma unroll
-            for (int b = 0; b < B; ++b)
+                for (int b = 0; b < B; ++b)
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    s[b][r] -= top;
+                    for (int r = 0; r < 16; ++r)
+                        s[b][r] -= top;
+            }
         }
 #pragma unroll
         for (int b = 0; b < B; ++b)
@@ -276,16 +278,14 @@ template <int DT, int DP> __global__ void __launch_bounds__(NF * 64, 1) attn_few
     const int lane = threadIdx.x & 63, h = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // (the heads of a piece, whose rows lie side by side, run at the same time)
-    int v = blockIdx.y * (int)GRID_ROW + blockIdx.x;
-    if (v >= p.n_wg)
-        return;
-    int u = p.by_hkv(v);
+    const int wg = blockIdx.y * (int)GRID_ROW + blockIdx.x;
+    int v = wg, u = p.by_hkv(v);
     const int hk = v, slot = p.by_split(u), piece = u;
 
     const AttnPlace place = attn_find_slot<32>(p.q_off, p.b, p.q_tokens, p.pack, slot, p.n_slots);
     const AttnSeq q = place.s, k = p.same ? q : attn_seq(p.k_off, place.i, p.k_tokens);
     const int first = (slot - place.first) * 32, rows = q.len * p.pack;
-    if (first < 0 || first >= rows)
+    if (wg >= p.n_wg || first < 0 || first >= rows)
         return;
     const int row = first + (lane & 31);
     int head = min(row, rows - 1);
@@ -322,7 +322,8 @@ template <int DT, int DP> __global__ void __launch_bounds__(NF * 64, 1) attn_few
 #pragma unroll
         for (int r = 0; r < 16; ++r)
             o[b][r] = 0.0f;
-    float top = NO_MAXIMUM;
+    float top = NO_MAXIMUM, less = 0.0f; // the maximum, and what is subtracted
+    uint64_t far = 0; // rows of the wavefront that are
     AttnSum sums = {0.0f, 0.0f};
     for (int j = 0; j < n; ++j) {
         const char *kt = ring + (j % RING) * 2 * TILE_BYTES, *vt = kt + TILE_BYTES;
@@ -352,22 +353,23 @@ template <int DT, int DP> __global__ void __launch_bounds__(NF * 64, 1) attn_few
         for (int r = 1; r < 16; ++r)
             m = fmaxf(m, s[r]);
         m = attn_halves_max(m);
-        if (__builtin_amdgcn_ballot_w64((m - top) * p.scale_log2 > LAZY)) {
+        if (far | __builtin_amdgcn_ballot_w64((m - top) * p.scale_log2 > LAZY)) {
             const float to = fmaxf(m, top), by = __builtin_amdgcn_exp2f((top - to) * p.scale_log2);
             top = to;
+            less = __builtin_fmaf(top, p.scale_log2, -LIFT<DT>);
             sums.scale(by);
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     o[b][r] *= by;
-        }
-        float less = __builtin_fmaf(top, p.scale_log2, -LIFT<DT>);
-        if (__builtin_amdgcn_ballot_w64(fabsf(less) > FAR)) {
-            less = -LIFT<DT>;
+            far = __builtin_amdgcn_ballot_w64(fabsf(less) > FAR);
+            if (far) {
+                less = -LIFT<DT>;
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                s[r] -= top;
+                for (int r = 0; r < 16; ++r)
+                    s[r] -= top;
+            }
         }
 #pragma unroll
         for (int r = 0; r < 16; ++r)

@@ -38,16 +38,14 @@ template <int DT, int DP> __global__ void __launch_bounds__(NW * 64, DP > 128 ? 
 
     const int lane = threadIdx.x & 63, h = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wg = blockIdx.y * (int)GRID_ROW + blockIdx.x;
-    if (wg >= p.n_wg)
-        return;
+    const int wg = blockIdx.y * (int)GRID_ROW + blockIdx.x; // (those from n_wg on leave below, with the slots that no sequence has: by then the wait for the arguments has passed)
     int v = xcd_grouped(wg, p.n_wg); // (as in the forward)
     const int hk = p.by_slots(v), slot = p.n_slots - 1 - v;
 
     const AttnPlace place = attn_find_slot<ROWS>(p.q_off, p.b, p.q_tokens, p.pack, slot, p.n_slots);
     const AttnSeq q = place.s, k = p.same ? q : attn_seq(p.k_off, place.i, p.k_tokens);
     const int first = (slot - place.first) * ROWS, rows = q.len * p.pack;
-    if (first < 0 || first >= rows)
+    if (wg >= p.n_wg || first < 0 || first >= rows)
         return;
 
     const int row = first + w * 32 + (lane & 31);
@@ -219,16 +217,14 @@ template <int DT, int DP> __global__ void __launch_bounds__(NK * 64, DP > 128 ? 
 
     const int lane = threadIdx.x & 63, h = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wg = blockIdx.y * (int)GRID_ROW + blockIdx.x;
-    if (wg >= p.n_wg)
-        return;
+    const int wg = blockIdx.y * (int)GRID_ROW + blockIdx.x; // (those from n_wg on leave below, with the slots that no sequence has: by then the wait for the arguments has passed)
     int v = xcd_grouped(wg, p.n_wg), x = p.by_split(v); // (the first tiles, which the most queries see under a causal mask, come first)
     const int piece = v, hk = p.by_slots(x), slot = x;
 
     const AttnPlace place = attn_find_slot<KEYS>(p.k_off, p.b, p.k_tokens, 1, slot, p.n_slots);
     const AttnSeq k = place.s, q = p.same ? k : attn_seq(p.q_off, place.i, p.q_tokens);
     const int first = (slot - place.first) * KEYS, ahead = k.len - q.len;
-    if (first < 0 || first >= k.len)
+    if (wg >= p.n_wg || first < 0 || first >= k.len)
         return;
     const int wave_key = first + w * 32, key = wave_key + (lane & 31);
     const uint64_t at = (uint32_t)(k.start + min(key, k.len - 1));
