@@ -289,15 +289,19 @@ int maxsim_rope(const void *X, int64_t tokens, int heads, int d, int64_t x_token
  *   Q, O  [q_tokens, hq, d],  K, V [k_tokens, hkv, d]   fp16 or bf16; query head h reads key head h / (hq / hkv)
  *   strides  HOST int64 [8]: token and head stride of Q, K, V, O in this order, multiples of 8 and token strides below
  *         2^24; NULL: all without gaps.  Base pointers are multiples of 16 bytes.
- *   q_offsets, k_offsets [b + 1] int32 (device), as doc_offsets in maxsim_forward_ragged; sequences may be empty
+ *   q_offsets, k_offsets [b + 1] int32 (device), as doc_offsets in maxsim_forward_ragged (they may be the same array); sequences may be
+ *         empty.  A sequence's keys end where the next one's begin: kept keys cannot grow in place.
  *   hq    a multiple of hkv;  d  a multiple of 8 up to 256;  10^-30 < scale < 10^30
  *   causal  nonzero: the last query sees all keys, the one before it all but the last, and so on
  *           (query t of lq sees keys j <= t + lk - lq).  Zero: all queries see all keys of their sequence.
  *   lse   [q_tokens, hq] float32 or NULL
  *   workspace  maxsim_attention_workspace(...) bytes (device, 16-byte aligned); may be NULL where that is 0
  * A query that sees no key gets O = 0 and lse = -inf.  Scores, the softmax's maximum and sum and the sums over keys are
- * fp32; probabilities are rounded to the inputs' type before they multiply V.  The result is the same on every
- * run.  What a sequence's rows hold does not reach another sequence's results.  O lies apart from the inputs.
+ * fp32; probabilities are rounded to the inputs' type before they multiply V (in fp16 to 2^-32 of the largest at
+ * the finest).  The result is the same on every run.  O lies apart from the inputs.
+ * Inputs are finite, as everywhere here.  One that is not stays in its sequence: lse of a query that sees such a key is NaN, never
+ * -inf, and another sequence's results are what they were.  Within the sequence a key behind the causal mask does not reach a
+ * query, but a value behind it has weight 0 in the products, which an infinity or a NaN does not survive.
  */
 int64_t maxsim_attention_workspace(int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, int hkv, int d);
 int maxsim_attention(const void *Q, const void *K, const void *V, const int64_t *strides, const int32_t *q_offsets,
@@ -313,8 +317,10 @@ int maxsim_attention(const void *Q, const void *K, const void *V, const int64_t 
  *   strides  HOST int64 [16]: token and head stride of Q, K, V, O, dO, dQ, dK, dV, as above; NULL: all without gaps
  *   workspace  maxsim_attention_backward_workspace(...) bytes (device, 16-byte aligned)
  * Sums are fp32 in a fixed order (no atomics): the same bits on every run.  P and dS are rounded to the inputs' type
- * before they enter the last products (dS in two parts for dQ of rows that see few keys), so that fp16 gradients want the usual
- * loss scale: what is below 6e-8 in dS is lost.  The gradients lie apart from the inputs and from each other.
+ * before they enter the last products (dS in two parts for dQ, except in causal rows of more than 512 keys whose sequence begins
+ * with its first query), so that fp16 gradients want the usual loss scale: what is below 3e-8 in P or dS is lost.  P is computed
+ * again from the scores and lse: it is as exact as fp32 is at the size of the scores (2^-24 of them, in the exponent).  The
+ * gradients lie apart from the inputs and from each other.
  */
 int64_t maxsim_attention_backward_workspace(int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, int hkv, int d);
 int maxsim_attention_backward(const void *Q, const void *K, const void *V, const void *O, const float *lse,
@@ -325,9 +331,10 @@ int maxsim_attention_backward(const void *Q, const void *K, const void *V, const
 
 /*
  * Clipping by the global norm:  norm = sqrt(sum of all gradients' squares),  out_i = min(1, max_norm / (norm + 1e-6)) g_i.
- *   grads, out  HOST arrays of n device pointers (out[i] may be grads[i]: in place); tensors without gaps, aligned to their elements
+ *   grads, out  HOST arrays of n device pointers (out[i] may be grads[i]: in place); tensors without gaps, aligned to their elements,
+ *               which otherwise lie apart from each other
  *   numel       HOST int64 [n], may be 0;  dtypes  HOST int32 [n], maxsim_dtype of grads[i] and out[i]
- *   norm        [1] float32 (device)
+ *   norm        [1] float32 (device); inf where the norm is beyond fp32 (the factor is right all the same)
  *   workspace   maxsim_clip_workspace(n) bytes (device, 16-byte aligned)
  * The arrays on the host may be reused when the call returns.  Squares are added in fp64 in a fixed order.  A gradient that
  * is not finite shows in the norm and, as in the formula, in every product with the factor 0 or NaN that it makes.

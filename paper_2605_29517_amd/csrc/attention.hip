@@ -27,7 +27,7 @@ constexpr float FAR = 1048576.0f;
 
 // The softmax's sum, of which a row has up to millions of terms that may round alike (equal keys): a step's terms are added as a tree, and the steps with
 // what the last addition lost. Added one by one, 2^17 equal keys put lse 226 times as far off as the rounding of the scores may; so it is half of
-// that, for 1 to 2 % of the time (250 short texts 71.2 -> 72.2 us, a long prompt 546 -> 547, heads of 256 146 -> 149).
+// that, for 1 to 2 % of the time (250 short texts 71.2 -> 72.2 us, a long prompt 546 -> 547, 16 x 1024 tokens of heads of 256 159 -> 162).
 struct AttnSum {
     float sum, lost; // sum - lost is the value
     __device__ __forceinline__ void add(float x)
@@ -94,9 +94,9 @@ template <int DT, int NB> __device__ __forceinline__ void attn_write(const AttnP
         p.lse[at] = lse;
 }
 
-// Long sequences are bound by the matrix units under the power limit: one causal prompt of 8192 tokens, 32 heads of 128 over 8, 508-518 us
-// (1060-1080 TFLOP/s; matrix units 59 % busy at 1.8 of 2.4 GHz), 16 x 1024 tokens of 8 heads of 256 over one 138 us (996). Short ones
-// are bound by latency and by the exponentials: 250 texts of 64 to 300 tokens, 12 heads of 64, 75 us. Two workgroups of four wavefronts to a
+// Long sequences are bound by the matrix units under the power limit: one causal prompt of 8192 tokens, 32 heads of 128 over 8, 519 us, 545 on a
+// warm card (1010-1060 TFLOP/s; compute units 93 % busy, their matrix units 59 % of that at 1.8 of 2.4 GHz), 16 x 1024 tokens of 8 heads of 256 over one 162 us (850).
+// Short ones are bound by latency and by the exponentials: 250 texts of 64 to 300 tokens, 12 heads of 64, 72-80 us. Two workgroups of four wavefronts to a
 // compute unit (four at d <= 64): eight wavefronts to a tile of K and V take 2 % off long sequences and put 7 % on such texts.
 // B, the blocks of 32 keys between two looks at the maximum: 2 hides more behind the products where the registers allow it (d = 128: prompt 518 us,
 // 523 with 1; 16 sequences of 9 to 130 new tokens 125 and 127; 500 texts of 150 tokens at d = 64 115 with 1, 122 with 2; d = 32 70 and 76).
@@ -265,7 +265,7 @@ template <int DT, int DP, int NW> __global__ void __launch_bounds__(NW * 64, DP 
 // rate. A wavefront owns all 32 rows of the workgroup and every NF-th tile of 32 keys of the piece, which it copies to a ring in
 // LDS of its own, RING tiles of K and of V ahead: nothing waits for another wavefront, and two workgroups keep 100 KB on their way to a compute
 // unit. The wavefronts' results are joined through LDS at the end. Bound by the memory: one token after each of 64 x 2048 .. 8192 keys, 8
-// heads of 128 (1.4 GB), 245 us, 5.9 TB/s; one token after 100003 keys of two heads (102 MB) 20.7 us and 6 for the join.
+// heads of 128 (1.4 GB), 244 us, 5.9 TB/s; one token after 100003 keys of two heads (102 MB) 20-21 us and 6 for the join.
 // Workgroups go round the XCDs one by one: in contiguous ranges, as in the other kernel, unequal sequences load the XCDs unequally
 // (16 sequences of 500 .. 16000 keys 117 us, 87 so; 32 x 4000 keys of 16 heads 181 and 164).
 constexpr int NF = 2;

@@ -7,9 +7,10 @@
 //   dK, dV  a workgroup owns keys and walks the queries of all heads that share them: S, dP, dV += P^T dO, dK += dS^T Q.
 // Scores and dP are thus computed twice, seven products instead of five (eight where dS is kept in two parts, nine in the exact pass); adding dQ
 // up from the second kernel would need an fp32 array of dQ and atomics. P and dS are rounded to the inputs' type for the last products (as P is
-// in the forward). Bound, as the forward, by the matrix units under the power limit where sequences are long: 4 x 4096 causal tokens of 32
-// heads of 128 over 8 take 750 us (dQ) and 1090-1200 (dK, dV; 57-64 % of the units' time at 1.8 GHz); 250 texts of 64 to 300 tokens, 12 heads of 64,
-// 115 and 118 us, bound by latency.
+// in the forward). dQ of long sequences is bound, as the forward, by the matrix units under the power limit: 4 x 4096 causal tokens of 32
+// heads of 128 over 8 take 750 us (compute units 92 % busy, their matrix units 61 % of that; 5 registers of 256 are spilled at d = 128, 12 in fp16, outside the loops). dK and dV of
+// these take 1160-1200, with compute units busy 78 % of the time: a sequence's key tiles go out before the next one's, and the last sequence's heaviest start late. 250 texts of
+// 64 to 300 tokens, 12 heads of 64, take 112-123 and 120-133 us, bound by latency and by reading Q, K, V and dO once in each kernel (85 us each at a copy's rate).
 #include "attention.h"
 
 namespace maxsim {
@@ -25,8 +26,8 @@ constexpr int Q_TILE = 32; // query rows per step of the dK, dV kernel
 // Under a causal mask rows of more than SPLIT_KEYS_CAUSAL keys bring little of the gradient beside the first rows, and stay as they are; not so where
 // keys are kept before the first row, which all see many then (256 rows of heads of 64 after 600 kept keys: 1.60 times without the
 // second part, 1.23 with it; the gradient of eight times 256 rows after 1244 to 3744 keys, 16 heads of 128 over 4, takes 235 us for 214).
-// What the last two cost: 500 texts
-// of 100 tokens, 16 heads of 128 over 4, 379 us of gradient without, 396 with; 64 x 1024 tokens of 12 heads of 64, no mask, 745 and 826.
+// What the last two of the three cost: 500 texts of 100 tokens, 16 heads of 128 over 4, 379 us of gradient without, 396 with; 64 x 1024 tokens of
+// 12 heads of 64, no mask, 745 and 826.
 constexpr int EXACT_KEYS = 128, SPLIT_KEYS_CAUSAL = 512;
 constexpr float LOG2E = 1.44269504088896341f;
 
@@ -218,7 +219,7 @@ template <int DT, int DP> __global__ void __launch_bounds__(NK * 64, DP > 128 ? 
     const int lane = threadIdx.x & 63, h = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wg = blockIdx.y * (int)GRID_ROW + blockIdx.x; // (those from n_wg on leave below, with the slots that no sequence has: by then the wait for the arguments has passed)
-    int v = xcd_grouped(wg, p.n_wg), x = p.by_split(v); // (the first tiles, which the most queries see under a causal mask, come first)
+    int v = xcd_grouped(wg, p.n_wg), x = p.by_split(v); // (of each sequence the first tiles, which the most queries see under a causal mask, come first)
     const int piece = v, hk = p.by_slots(x), slot = x;
 
     const AttnPlace place = attn_find_slot<KEYS>(p.k_off, p.b, p.k_tokens, 1, slot, p.n_slots);

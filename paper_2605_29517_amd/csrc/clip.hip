@@ -2,12 +2,12 @@
 //
 // Two passes over the gradients, which is what the definition needs: one for the sum, one for the product. The tensors are cut into
 // chunks of CHUNK entries, and every workgroup takes a contiguous range of the chunks of all tensors, so that many small
-// tensors and a few large ones fill the chip alike. Squares are added in 64 bits (no overflow at any fp32 value; the adders keep up
-// with the memory four times over), each workgroup's sum goes to a place of its own and the second pass adds these in a
+// tensors and a few large ones fill the chip alike. Squares are added in 64 bits (no overflow at any fp32 value, nor in the factor, where the norm itself is beyond fp32;
+// the adders keep up with the memory four times over), each workgroup's sum goes to a place of its own and the second pass adds these in a
 // fixed order in every workgroup: the same bits every time, without atomics or a launch in between. The second pass walks its range
 // backwards: what the first one read last is what the caches still hold.
 //
-// Bound by the memory: 5.2 GB of fp32 take 2820 us (sum 760, 6.9 TB/s; product 2040, 5.1); 22 MB, which stay in the caches, 18.5 us in two launches.
+// Bound by the memory: 5.2 GB of fp32 take 2840 us (sum 760, 6.9 TB/s; product 2050, 5.1); 22 MB, which stay in the caches, 18.6 us in two launches.
 //
 // Compiled with NaNs honoured: a gradient that is not finite has to show in the norm.
 #include <algorithm>

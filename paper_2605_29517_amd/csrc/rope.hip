@@ -3,7 +3,7 @@
 // Each entry is read once and written once; what else there is to do is one angle per (token, pair), shared by the token's heads. A
 // workgroup takes some tokens, puts their cosines and sines into LDS, and then moves chunks of 16 bytes through registers. The angle is
 // reduced in 64 bits (its fraction of a turn), so that positions of 10^6 keep the accuracy of small ones. Bound by the memory: 16 x 1024
-// tokens of 40 heads of 128, bf16 (336 MB), 54.6 us, 6.1 TB/s; fp32 texts of 1.1 GB 189 us, 5.9; a few tokens (32 of 16 heads of 64, fp16) by
+// tokens of 40 heads of 128, bf16 (336 MB), 54.8 us, 6.1 TB/s; fp32 texts of 1.1 GB 189 us, 5.9; a few tokens (32 of 16 heads of 64, fp16) by
 // the launch, 3.1 us.
 #include <algorithm>
 
@@ -72,6 +72,7 @@ enum RopePairs { HALVES, HALVES_ANY, NEIGHBOURS, SINGLE };
 // lane takes one chunk and reads the partners of its entries from where they lie, so that a head's row is read twice, the second time
 // from the cache. NEIGHBOURS: pairs lie inside a chunk. SINGLE (V = 1): a lane takes one pair or one plain entry, wherever they lie.
 // 30000 tokens of 16 heads, bf16: d = 128 HALVES 40.6 us, HALVES_ANY 51.6; neighbours 43.2, SINGLE 82.4; 36 of 64 entries HALVES_ANY 32.6, SINGLE 70.2.
+// In place, HALVES_ANY could read a partner that another lane has already turned: SINGLE, whose lanes hold both.
 template <int DT, int V, RopePairs PAIRS, bool ONCE> __global__ void __launch_bounds__(WG) rope_kernel(RopeParams p)
 {
     typedef typename Elem<DT>::T T;
