@@ -299,9 +299,9 @@ int maxsim_rope(const void *X, int64_t tokens, int heads, int d, int64_t x_token
  * A query that sees no key gets O = 0 and lse = -inf.  Scores, the softmax's maximum and sum and the sums over keys are
  * fp32; probabilities are rounded to the inputs' type before they multiply V (in fp16 to 2^-32 of the largest at
  * the finest).  The result is the same on every run.  O lies apart from the inputs.
- * Inputs are finite, as everywhere here.  One that is not stays in its sequence: lse of a query that sees such a key is NaN, never
- * -inf, and another sequence's results are what they were.  Within the sequence a key behind the causal mask does not reach a
- * query, but a value behind it has weight 0 in the products, which an infinity or a NaN does not survive.
+ * Inputs are finite, as everywhere here.  What is not stays in its sequence: another sequence's results are what they were, and
+ * a NaN among the keys that a query sees makes its lse NaN.  Within the sequence a key behind the causal mask does not
+ * reach a query, but a value behind it has weight 0 in the products, which an infinity or a NaN does not survive.
  */
 int64_t maxsim_attention_workspace(int64_t b, int64_t q_tokens, int64_t k_tokens, int hq, int hkv, int d);
 int maxsim_attention(const void *Q, const void *K, const void *V, const int64_t *strides, const int32_t *q_offsets,
