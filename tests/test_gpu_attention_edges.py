@@ -1,5 +1,4 @@
 """maxsim_attention and maxsim_attention_backward where sizes, layouts and numbers are at their ends."""
-import math
 import os
 import sys
 
