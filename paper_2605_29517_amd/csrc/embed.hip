@@ -897,12 +897,6 @@ struct SortPlan {
     int64_t rows; // places in the order
 };
 constexpr int64_t SCAN_TOKENS = 8192;
-// All in one launch, where the ids of a range may all be tokens of one workgroup, which adds them up alone: 1440 tokens of 256, fp32, 7.6 us, in three launches 13.6; 4000 of 256, bf16,
-// vocabulary 50001, 13 and 21, half of them one id 26 and 23. Beyond 2 MB that id would cost too much (4000 of 1024, bf16: 14 and 17, half of them one id 56 and 22).
-bool is_small(int64_t n, int64_t vocab, int d, int size, int w_size)
-{
-    return n <= SMALL_TOKENS && n * d * size <= (2 << 20) && vocab * d * w_size < PAST_CACHES && (vocab + 255) / 256 <= MAX_RANGE;
-}
 SortPlan sort_plan(int64_t n, int64_t vocab, int d)
 {
     SortPlan s;
@@ -926,6 +920,16 @@ SortPlan sort_plan(int64_t n, int64_t vocab, int d)
     }
     return s;
 }
+// All in one launch, where the ids of a range may all be tokens of one workgroup, which adds them up alone: 1440 tokens of 256, fp32, 7.6 us, in three launches 13.6; 4000 of 256, bf16,
+// vocabulary 50001, 13 and 21, half of them one id 26 and 23. Beyond 2 MB that id would cost too much (4000 of 1024, bf16: 14 and 17, half of them one id 56 and 22).
+// A workgroup takes all pieces of its range's rows at once: where their indices do not divide (wide rows of single entries), the other kernels take a row at a time.
+bool is_small(const SortPlan &s, int64_t n, int64_t vocab, int d, int size, int w_size, int chunks)
+{
+    return n <= SMALL_TOKENS && n * d * size <= (2 << 20) && vocab * d * w_size < PAST_CACHES && (vocab + 255) / 256 <= MAX_RANGE &&
+           Divisor::divides_below((int64_t)s.range * chunks, chunks);
+}
+// Entries of a piece of dW: added to what is there, the pieces of a row may not overlap
+int entries_of_piece(int d, int full, bool accumulate) { return d >= full && !(accumulate && d % full != 0) ? full : 1; }
 int64_t up16(int64_t x) { return (x + 15) / 16 * 16; }
 
 } // namespace
@@ -971,7 +975,8 @@ hipError_t embed_backward_launch(const void *dY, int dtype, const void *tokens, 
     int32_t *row_start = reinterpret_cast<int32_t *>(ws), *at = reinterpret_cast<int32_t *>(ws + up16(4 * (rows + 1))), *key = at + up16(4 * n) / 4;
     float *part = reinterpret_cast<float *>(key + up16(4 * n) / 4);
     const Order order = s.dealt ? Order{s.block, s.ranges, s.range, Divisor((uint32_t)s.ranges), Divisor((uint32_t)s.range)} : Order{0, 0, 0, Divisor(1), Divisor(1)};
-    const bool small = is_small(n, vocab, d, dtype == MAXSIM_F32 ? 4 : 2, w_dtype == MAXSIM_F32 ? 4 : 2);
+    const int piece = entries_of_piece(d, dtype == MAXSIM_F32 || w_dtype == MAXSIM_F32 ? 4 : 8, accumulate), chunks = (d + piece - 1) / piece;
+    const bool small = is_small(s, n, vocab, d, dtype == MAXSIM_F32 ? 4 : 2, w_dtype == MAXSIM_F32 ? 4 : 2, chunks);
     const SortParams scan = {tokens, n, (uint32_t)vocab, (uint32_t)rows, order, s.range, row_start, at, key};
     if (small) {
         // (sorts by itself)
@@ -998,7 +1003,7 @@ hipError_t embed_backward_launch(const void *dY, int dtype, const void *tokens, 
             constexpr int FROM = decltype(from)::value, TO = decltype(to)::value, FULL = FROM == MAXSIM_F32 || TO == MAXSIM_F32 ? 4 : 8;
             auto go = [&](auto v) {
                 constexpr int V = decltype(v)::value;
-                const int slice = slice_of(n, d), chunks = (d + V - 1) / V, per = rows_per_wg(rows, chunks);
+                const int slice = slice_of(n, d), per = rows_per_wg(rows, chunks);
                 const int slices = n > slice ? (int)((n + slice - 1) / slice) : 0, slices_per = std::max(1, WG / chunks), slice_wgs = (slices + slices_per - 1) / slices_per;
                 const SumParams p = {dY, dW, row_start, at, key, part, (uint32_t)vocab, (uint32_t)rows, order, d, slice, slices, chunks, per, slices_per, Divisor((uint32_t)chunks), slice_wgs, accumulate, scale};
                 if (small) {
@@ -1017,8 +1022,7 @@ hipError_t embed_backward_launch(const void *dY, int dtype, const void *tokens, 
                     embed_join_kernel<TO, V><<<(unsigned)slices, JOIN_WG, 0, stream>>>(p);
                 return hipGetLastError();
             };
-            // (added to what is there, the pieces of a row may not overlap)
-            return d >= FULL && !(accumulate && d % FULL != 0) ? go(std::integral_constant<int, FULL>{}) : go(std::integral_constant<int, 1>{});
+            return piece == FULL ? go(std::integral_constant<int, FULL>{}) : go(std::integral_constant<int, 1>{});
         });
     });
 }
