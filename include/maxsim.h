@@ -402,7 +402,7 @@ int maxsim_norm_rope_backward(const void *X, const void *dY, int64_t tokens, int
  *   index    [n, k] int32 or NULL (k = b: entry e is column e);  1 <= k <= 1024, b < 2^31;  10^-30 < tau < 10^30
  *   maxsim_distill           loss [n] float32;  lse [n] float32 or NULL: log sum_j exp(scores[i, j] / tau)
  *   maxsim_distill_backward  g [n, b] dtype, rows g_stride apart = dloss[i] * d loss[i] / d scores;  lse as maxsim_distill left it;  dloss [n] float32.
- *                            q is as exact as fp32 is at the size of lse (2^-24 of it, in the exponent)
+ *                            The rows' sums are formed again, so that q is as exact as maxsim_distill_grad's (fp32's lse would cost it 2^-24 of lse's size)
  *   maxsim_distill_grad      both at once: g = weight * d loss[i] / d scores (weight: 1 / n for the mean, a loss scale);  loss [n] or NULL
  *   g may be scores itself, with its stride (and is otherwise apart from the inputs)
  *   workspace  maxsim_distill_workspace(n, b, dtype) bytes (device, 16-byte aligned; NULL where that is 0)

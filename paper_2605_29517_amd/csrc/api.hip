@@ -824,7 +824,7 @@ int maxsim_distill_backward(const void *scores, int n, int64_t b, int64_t stride
         return MAXSIM_ERR_UNSUPPORTED;
     if (int rc = ensure_init())
         return rc;
-    return finish(maxsim::distill_launch(scores, n, (int)b, stride, (int)dtype, teacher, (int)t_dtype, index, k, tau, nullptr, const_cast<float *>(lse), dloss, 0.0f, g, g_stride,
+    return finish(maxsim::distill_launch(scores, n, (int)b, stride, (int)dtype, teacher, (int)t_dtype, index, k, tau, nullptr, nullptr, dloss, 0.0f, g, g_stride,
                                          nullptr, num_cu(), static_cast<hipStream_t>(stream)));
 }
 
