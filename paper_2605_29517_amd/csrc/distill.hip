@@ -241,10 +241,10 @@ template <int DT, int V, DistillMode MODE, int TH, int KEEP, bool ONCE> __global
     typedef typename Elem<DT>::T T;
     extern __shared__ char lds[];
     const int groups = blockDim.x / TH, group = TH > 64 ? 0 : __builtin_amdgcn_readfirstlane((int)(threadIdx.x / TH)), tid = threadIdx.x % TH;
-    const int64_t unit = (int64_t)blockIdx.x * groups + group;
+    const int64_t wg = (int64_t)blockIdx.y * GRID_ROW + blockIdx.x, unit = wg * groups + group;
     const bool parts = MODE == GRAD && TH > 64 && p.pieces > 1; // (a loss takes the parts' sums alone)
-    const int64_t i = parts ? (int64_t)(blockIdx.x / (unsigned)p.pieces) : unit;
-    const int part = parts ? (int)(blockIdx.x % (unsigned)p.pieces) : 0;
+    const int64_t i = parts ? (int64_t)((unsigned)wg / (unsigned)p.pieces) : unit; // (of few rows: fewer than 2^32)
+    const int part = parts ? (int)((unsigned)wg % (unsigned)p.pieces) : 0;
     if (i >= p.n)
         return; // (the whole group)
     const int k = p.k, b = p.b;
@@ -476,7 +476,7 @@ template <int DT, int V, DistillMode MODE, int TH, int KEEP> hipError_t go(const
     const int groups = TH > 64 ? 1 : p.n > 1024 ? 4 : 1;
     const size_t lds = (TH > 64 ? 24 * (TH / 64) + 12 * (size_t)p.slots : 0) + 12 * (size_t)p.k * groups;
     const int64_t units = (int64_t)p.n * (TH > 64 ? MODE == LOSS ? 1 : p.pieces : 1);
-    const dim3 grid((unsigned)((units + groups - 1) / groups));
+    const dim3 grid = grid_rows((units + groups - 1) / groups);
     const int64_t bytes = (int64_t)p.n * p.b * (int64_t)sizeof(typename Elem<DT>::T) * (MODE == LOSS ? 1 : 2);
     if (TH > 64 && bytes >= PAST_CACHES)
         distill_kernel<DT, V, MODE, TH, KEEP, (TH > 64)><<<grid, TH * groups, lds, stream>>>(p);

@@ -1,5 +1,5 @@
-"""What the host code of the embedding's gradient launches, and whether its kernels' arithmetic of indices holds there: the host code by itself, whose launches are
-looked at instead of made (no GPU needed)."""
+"""What the host code of the embedding's gradient and of distillation launches, and whether the grids and the kernels' arithmetic of indices hold there: the host code
+by itself, whose launches are looked at instead of made (no GPU needed)."""
 import os
 import subprocess
 
@@ -116,6 +116,30 @@ int main()
 """
 
 
+DISTILL = r"""
+#include "%(csrc)s/distill.hip"
+""" + RUNTIME + r"""
+using namespace maxsim;
+static void look(const std::string &kernel, dim3 grid, dim3 block, void **args)
+{
+    const DistillParams &p = *static_cast<DistillParams *>(args[0]);
+    printf("%%s %%lu %%lu %%u %%d ", kernel.find("stats") != std::string::npos ? "stats" : "rows", (unsigned long)grid.x, (unsigned long)grid.y * grid.z, block.x, p.pieces);
+}
+int main()
+{
+    static float any[4], out[4];
+    long n, b;
+    int k, dtype, indexed, how;
+    while (scanf("%%ld %%ld %%d %%d %%d %%d", &n, &b, &k, &dtype, &indexed, &how) == 6) {
+        const hipError_t e = distill_launch(any, (int)n, (int)b, b, dtype, any, dtype, indexed ? reinterpret_cast<int32_t *>(any) : nullptr, k, 1.0f, any, nullptr, how == 2 ? any : nullptr, 1.0f,
+                                            how ? out : nullptr, b, any, 256, nullptr);
+        printf("%%s\n", e == hipSuccess ? "" : "error");
+    }
+    return 0;
+}
+"""
+
+
 def program(tmp_path_factory, name, text):
     at = tmp_path_factory.mktemp(name)
     (at / "harness.hip").write_text(text % {"csrc": B.CSRC})
@@ -157,3 +181,25 @@ def test_quotients(embed):
 def test_one_launch_for_few_tokens(embed):
     for call in ((1440, 1000, 256, F32, F32, 0), (1440, 1000, 256, F32, F32, 1), (40, 5000, 1023, F16, F16, 1), (20, 1000, 8191, F16, F16, 1)):
         assert embed([call])[0][::2] == ["small"], call
+
+
+@pytest.fixture(scope="module")
+def distill(tmp_path_factory):
+    """(n, b, k, dtype, whether columns are named, what: 0 the losses, 1 both, 2 the gradient) -> kernels by name, each followed by its grid's row, rows, the workgroup's threads and the
+    parts of a row."""
+    return program(tmp_path_factory, "distill", DISTILL)
+
+
+@pytest.mark.parametrize("how", [0, 1, 2])
+def test_as_many_rows_as_there_are(distill, how):
+    """A row of a grid holds fewer than 2^32 threads, and the grid covers all rows: 2^31 - 1 short ones, too."""
+    calls = [(n, b, min(k, b), dtype, indexed, how) for n in (1, 3, 255, 256, 5000, (1 << 22) + 1, (1 << 24) - 1, 1 << 24, (1 << 26) - 1, 1 << 26, (1 << 28) + 3, (1 << 31) - 1)
+             for b, k, indexed in ((2, 2, 0), (9, 3, 1), (300, 200, 1), (1000, 1000, 0), (2100, 20, 1), (5000, 130, 1), (20_000, 7, 1), (70_000, 7, 1)) for dtype in (F32, F16) if n * b < 1 << 38]
+    for call, r in zip(calls, distill(calls)):
+        assert "error" not in r and len(r) in (5, 10), call
+        for name, x, y, threads, pieces in zip(*(r[i::5] for i in range(5))):
+            x, y, threads, pieces = int(x), int(y), int(threads), int(pieces)
+            assert 0 < x * threads < 1 << 32 and y < 1 << 16, (call, name, x, y, threads)
+            units = call[0] * (pieces if name == "stats" or how else 1)
+            groups = -(-units // (x * y))  # of a workgroup, each with a row
+            assert groups == 1 or threads // 64 >= groups, (call, name)
