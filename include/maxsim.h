@@ -349,7 +349,7 @@ int maxsim_clip_grad_norm(const void *const *grads, void *const *out, const int6
  *     Y[t] = scale W[v(t)],    dW[v] = scale * (sum over the tokens t with v(t) = v of dY[t])
  *   W, dW   [vocab, d] dtype / w_dtype    Y, dY [n, d] y_dtype / dtype    any types: fp32 weights may give 16-bit activations
  *   tokens  [n] int32 or int64 (device; token_bytes 4 or 8)   an id outside [0, vocab) names no row (padding): Y[t] = 0, and no gradient
- *   n < 2^31 (the gradient: 2^27), vocab < 2^31 - 1, d <= 65536
+ *   n < 2^31 (the gradient: 2^27), vocab < 2^31 - 1, d <= 65536; of more than 49152 tokens the gradient takes 2^19 ids at a time, with four launches for each
  *   accumulate  nonzero: dW += (rows that do not occur are not touched); zero: every row is written, zeros where no token is
  *   workspace   maxsim_embed_backward_workspace(...) bytes (device, 16-byte aligned)
  * Pointers are aligned to their elements (rows of 16-byte multiples are fastest).  Products and sums are fp32, rounded once; a row's

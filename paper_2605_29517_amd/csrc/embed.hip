@@ -35,14 +35,15 @@ struct LookupParams {
     float scale;
 };
 
-// The id of a token as 32 bits, 2^32 - 1 where it names no row
-template <bool WIDE> __device__ __forceinline__ uint32_t token_id(const void *tokens, int64_t t, uint32_t vocab)
+// The id of a token, counted from the id `first` on, as 32 bits, 2^32 - 1 where it names none of the `vocab` rows from there (first + vocab < 2^31: what lies before them, negative ids
+// and those beyond the table are `vocab` or more away)
+template <bool WIDE> __device__ __forceinline__ uint32_t token_id(const void *tokens, int64_t t, uint32_t vocab, uint32_t first = 0)
 {
     if constexpr (WIDE) {
-        const uint64_t v = static_cast<const uint64_t *>(tokens)[t];
+        const uint64_t v = static_cast<const uint64_t *>(tokens)[t] - first;
         return v < vocab ? (uint32_t)v : 0xffffffffu;
     } else {
-        const uint32_t v = static_cast<const uint32_t *>(tokens)[t];
+        const uint32_t v = static_cast<const uint32_t *>(tokens)[t] - first;
         return v < vocab ? v : 0xffffffffu;
     }
 }
@@ -215,11 +216,11 @@ struct Scan {
     int32_t part[SORT_WAVES], below[SORT_WAVES];
 };
 
-// f(to, position, place in the range) for all tokens of this workgroup's range of `rows` places, by place and, within one, in order, counted from
+// f(to, position, place in the range) for all tokens of a workgroup's range of `rows` places, by place and, within one, in order, counted from
 // what `starts` gave back: starts(tokens of the ranges before, of thread r: where place r begins, how many it has).
-template <bool WIDE, class Starts, class F> __device__ __forceinline__ void scan_range(const SortParams &p, Scan &s, uint32_t rows, Starts starts, F f)
+template <bool WIDE, class Starts, class F> __device__ __forceinline__ void scan_range(const SortParams &p, Scan &s, uint32_t range, uint32_t rows, Starts starts, F f)
 {
-    const uint32_t range = blockIdx.x, lo = range * (uint32_t)p.range;
+    const uint32_t lo = range * (uint32_t)p.range;
     // whether an id is of the range, its place there, whether it is of a range before
     auto look = [&](uint32_t v, uint32_t &r, bool &before) {
         if (p.order.ranges == 0) {
@@ -320,12 +321,16 @@ template <bool WIDE, class Starts, class F> __device__ __forceinline__ void scan
     }
 }
 
+constexpr uint32_t SCAN_ROW = 1 << 21; // workgroups of a row of the grid, which holds fewer than 2^32 threads
 template <bool WIDE> __global__ void __launch_bounds__(SORT_WG) embed_scan_kernel(SortParams p)
 {
     __shared__ Scan s;
-    const uint32_t lo = blockIdx.x * (uint32_t)p.range, rows = p.rows - lo < (uint32_t)p.range ? p.rows - lo : (uint32_t)p.range;
+    const uint32_t range = blockIdx.y * SCAN_ROW + blockIdx.x, lo = range * (uint32_t)p.range; // (below 2^32 in the grid's last row, too)
+    if (lo >= p.rows)
+        return;
+    const uint32_t rows = p.rows - lo < (uint32_t)p.range ? p.rows - lo : (uint32_t)p.range;
     scan_range<WIDE>(
-        p, s, rows,
+        p, s, range, rows,
         [&](int base, int start, int n) {
             if (threadIdx.x < rows) {
                 p.row_start[lo + threadIdx.x] = base + start;
@@ -344,12 +349,11 @@ constexpr int SPLIT_WG = 512;
 constexpr int SPLIT_WAVES = SPLIT_WG / 64;
 constexpr int MAX_RANGES = 1024, RANGES_BITS = 10;
 constexpr int MAX_CHUNKS = 1024;
-constexpr int MAX_CHUNK = 1 << 14;
 
 struct SplitParams {
     const void *tokens;
     int64_t n;
-    uint32_t vocab;
+    uint32_t first, vocab; // the ids from the first one on
     int chunk, chunks;   // tokens of a chunk: a multiple of 4 SPLIT_WG
     Order order;
     uint32_t *list;      // [chunks][chunk] of every chunk, its tokens by range and in order: (position in the chunk, id in the range)
@@ -374,7 +378,7 @@ template <bool WIDE> __global__ void __launch_bounds__(SPLIT_WG) embed_split_ker
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t t = chunk0 + w * run + i + 64 * u + lane;
-            v[u] = token_id<WIDE>(p.tokens, t < p.n ? t : p.n - 1, p.vocab);
+            v[u] = token_id<WIDE>(p.tokens, t < p.n ? t : p.n - 1, p.vocab, p.first);
             v[u] = t < p.n ? v[u] : 0xffffffffu;
         }
     };
@@ -682,7 +686,7 @@ template <int FROM, int TO, int V, bool WIDE> __global__ void __launch_bounds__(
     if (tid == 0)
         longs = 0;
     scan_range<WIDE>(
-        sort, lds.scan, rows,
+        sort, lds.scan, blockIdx.x, rows,
         [&](int, int start, int n) {
             if (tid < (int)rows) {
                 first[tid] = start;
@@ -889,23 +893,27 @@ int rows_per_wg(int64_t rows, int chunks)
 // 32 72, 16 90; 262144 of 1024: 128 191 us, 64 204, 256 204; 12600 of 168, whose pieces take few threads: 16 30 us, 64 35)
 int slice_of(int64_t n, int d) { return n * d < (1 << 23) ? 16 : n < (1 << 17) ? 64 : 128; }
 
-// How the positions are sorted: in chunks, where there are more tokens than a look by every workgroup pays for and the ranges are few enough
+// How the positions are sorted: in chunks, where there are more tokens than a look by every workgroup pays for. More than MAX_IDS ids are taken some at a time, each with launches of its
+// own, unless the tokens are few: every workgroup's look takes a time in proportion to tokens times ids (rows of 4, bf16, 20000 tokens, 700000 ids: 46 us, in two parts 61; 10^7 ids 357 and 551;
+// 50000 tokens 77 and 66, 632 and 602; 300000 tokens 363 and 174; 10^6 tokens 1409 and 467).
 struct SortPlan {
     bool split;
     bool dealt; // ids to the ranges in turn
     int range, ranges, block, chunk, chunks; // block: of the order, a power of two
     int64_t rows; // places in the order
 };
-constexpr int64_t SCAN_TOKENS = 8192;
+constexpr int64_t SCAN_TOKENS = 8192, SCAN_TOKENS_OF_MANY_IDS = 49152;
+constexpr int64_t MAX_IDS = MAX_RANGE * MAX_RANGES;
+int64_t ids_at_a_time(int64_t n, int64_t vocab) { return n > SCAN_TOKENS_OF_MANY_IDS ? std::min(vocab, MAX_IDS) : vocab; }
 SortPlan sort_plan(int64_t n, int64_t vocab, int d)
 {
     SortPlan s;
     s.range = (int)std::min<int64_t>(MAX_RANGE, (vocab + 255) / 256);
     s.ranges = (int)((vocab + s.range - 1) / s.range);
     s.chunk = 4 * SPLIT_WG;
-    while (s.chunk < MAX_CHUNK && (n + s.chunk - 1) / s.chunk > MAX_CHUNKS)
+    while ((n + s.chunk - 1) / s.chunk > MAX_CHUNKS) // (2^17 tokens at most: a position in a chunk and a place in a range share 32 bits)
         s.chunk *= 2;
-    s.split = n > SCAN_TOKENS && s.ranges <= MAX_RANGES && (n + s.chunk - 1) / s.chunk <= MAX_CHUNKS;
+    s.split = n > SCAN_TOKENS && s.ranges <= MAX_RANGES;
     s.chunks = s.split ? (int)((n + s.chunk - 1) / s.chunk) : 0;
     s.dealt = s.ranges <= MAX_RANGES;
     s.block = 0;
@@ -960,14 +968,15 @@ hipError_t embed_launch(const void *W, int64_t vocab, int d, int dtype, const vo
 
 int64_t embed_backward_workspace(int64_t n, int64_t vocab, int d)
 {
-    const SortPlan s = sort_plan(n, vocab, d);
+    const SortPlan s = sort_plan(n, ids_at_a_time(n, vocab), d);
     const int64_t slices = (n + slice_of(n, d) - 1) / slice_of(n, d), sums = slices > 1 ? 8 * slices * d : 0;
     // (the chunks' lists are done with when the slices' sums begin)
     return up16(4 * (s.rows + 1)) + 2 * up16(4 * n) + std::max(sums, s.split ? 4 * (int64_t)s.chunks * (s.chunk + s.ranges + 1) : 0);
 }
 
-hipError_t embed_backward_launch(const void *dY, int dtype, const void *tokens, bool wide, int64_t n, int64_t vocab, int d, float scale, bool accumulate, void *dW, int w_dtype,
-                                 void *workspace, hipStream_t stream)
+// dW's `vocab` rows from the id `first` on
+static hipError_t some_rows(const void *dY, int dtype, const void *tokens, bool wide, int64_t n, int64_t first, int64_t vocab, int d, float scale, bool accumulate, void *dW, int w_dtype,
+                            void *workspace, hipStream_t stream)
 {
     char *ws = static_cast<char *>(workspace);
     const SortPlan s = sort_plan(n, vocab, d);
@@ -983,17 +992,18 @@ hipError_t embed_backward_launch(const void *dY, int dtype, const void *tokens, 
     } else if (s.split) {
         uint32_t *list = reinterpret_cast<uint32_t *>(part);
         int32_t *begin = reinterpret_cast<int32_t *>(list + (int64_t)s.chunks * s.chunk);
-        const SplitParams p = {tokens, n, (uint32_t)vocab, s.chunk, s.chunks, order, list, begin, row_start, at, key};
+        const SplitParams p = {tokens, n, (uint32_t)first, (uint32_t)vocab, s.chunk, s.chunks, order, list, begin, row_start, at, key};
         if (wide)
             embed_split_kernel<true><<<(unsigned)s.chunks, SPLIT_WG, 0, stream>>>(p);
         else
             embed_split_kernel<false><<<(unsigned)s.chunks, SPLIT_WG, 0, stream>>>(p);
         embed_place_kernel<<<(unsigned)s.ranges, SORT_WG, 0, stream>>>(p);
     } else {
+        const dim3 grid(std::min((unsigned)s.ranges, SCAN_ROW), ((unsigned)s.ranges + SCAN_ROW - 1) / SCAN_ROW);
         if (wide)
-            embed_scan_kernel<true><<<(unsigned)s.ranges, SORT_WG, 0, stream>>>(scan);
+            embed_scan_kernel<true><<<grid, SORT_WG, 0, stream>>>(scan);
         else
-            embed_scan_kernel<false><<<(unsigned)s.ranges, SORT_WG, 0, stream>>>(scan);
+            embed_scan_kernel<false><<<grid, SORT_WG, 0, stream>>>(scan);
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess)
@@ -1025,6 +1035,18 @@ hipError_t embed_backward_launch(const void *dY, int dtype, const void *tokens, 
             return piece == FULL ? go(std::integral_constant<int, FULL>{}) : go(std::integral_constant<int, 1>{});
         });
     });
+}
+
+hipError_t embed_backward_launch(const void *dY, int dtype, const void *tokens, bool wide, int64_t n, int64_t vocab, int d, float scale, bool accumulate, void *dW, int w_dtype,
+                                 void *workspace, hipStream_t stream)
+{
+    const int64_t ids = ids_at_a_time(n, vocab), row = (int64_t)d * (w_dtype == MAXSIM_F32 ? 4 : 2);
+    for (int64_t first = 0; first < vocab; first += ids) {
+        const hipError_t e = some_rows(dY, dtype, tokens, wide, n, first, std::min(ids, vocab - first), d, scale, accumulate, static_cast<char *>(dW) + first * row, w_dtype, workspace, stream);
+        if (e != hipSuccess)
+            return e;
+    }
+    return hipSuccess;
 }
 
 } // namespace maxsim

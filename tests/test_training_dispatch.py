@@ -59,6 +59,7 @@ EMBED = r"""
 #include "%(csrc)s/embed.hip"
 """ + RUNTIME + r"""
 using namespace maxsim;
+static uint64_t looks; // at tokens, of all workgroups that sort
 // Whether the quotients of all x below n are right: at the largest x of which the remainder is the largest they go wrong first.
 static bool right(const Divisor &y, int64_t n)
 {
@@ -72,32 +73,35 @@ static bool right(const Order &o, int64_t vocab, int64_t rows) { return o.ranges
 static void look(const std::string &kernel, dim3 grid, dim3 block, void **args)
 {
     const char *name = "";
-    bool ok = true;
+    bool ok = (uint64_t)grid.x * block.x < uint64_t(1) << 32 && grid.y < 1u << 16;
+    const uint64_t wgs = (uint64_t)grid.x * grid.y;
     if (kernel.find("embed_small") != std::string::npos) {
         const SortParams &s = *static_cast<SortParams *>(args[0]);
         const SumParams &p = *static_cast<SumParams *>(args[1]);
         name = "small";
-        ok = right(p.by_chunks, (int64_t)s.range * p.chunks) && right(p.order, p.vocab, p.rows);
+        ok = ok && right(p.by_chunks, (int64_t)s.range * p.chunks) && right(p.order, p.vocab, p.rows);
     } else if (kernel.find("embed_scan") != std::string::npos) {
         const SortParams &s = *static_cast<SortParams *>(args[0]);
         name = "scan";
-        ok = right(s.order, s.vocab, s.rows);
+        looks += wgs * s.n;
+        ok = ok && right(s.order, s.vocab, s.rows);
     } else if (kernel.find("embed_split") != std::string::npos || kernel.find("embed_place") != std::string::npos) {
         const SplitParams &s = *static_cast<SplitParams *>(args[0]);
         name = kernel.find("embed_split") != std::string::npos ? "split" : "place";
-        ok = right(s.order, s.vocab, (int64_t)s.order.range * s.order.ranges);
+        looks += s.n;
+        ok = ok && right(s.order, s.vocab, (int64_t)s.order.range * s.order.ranges);
     } else if (kernel.find("embed_sum") != std::string::npos) {
         const SumParams &p = *static_cast<SumParams *>(args[0]);
         name = "sum";
-        ok = right(p.by_chunks, (int64_t)p.per_wg * p.chunks) && right(p.by_chunks, (int64_t)p.slices_per_wg * p.chunks) && right(p.order, p.vocab, p.rows);
+        ok = ok && right(p.by_chunks, (int64_t)p.per_wg * p.chunks) && right(p.by_chunks, (int64_t)p.slices_per_wg * p.chunks) && right(p.order, p.vocab, p.rows);
     } else if (kernel.find("embed_join") != std::string::npos) {
         const SumParams &p = *static_cast<SumParams *>(args[0]);
         name = "join";
-        ok = right(p.order, p.vocab, p.rows);
+        ok = ok && right(p.order, p.vocab, p.rows);
     } else {
         const LookupParams &p = *static_cast<LookupParams *>(args[0]);
         name = "lookup";
-        ok = right(p.by_chunks, (int64_t)p.per_wg * p.chunks);
+        ok = ok && right(p.by_chunks, (int64_t)p.per_wg * p.chunks);
     }
     printf("%%s %%d ", name, ok);
 }
@@ -109,7 +113,8 @@ int main()
     while (scanf("%%ld %%ld %%d %%d %%d %%d", &n, &vocab, &d, &dtype, &w_dtype, &accumulate) == 6) {
         const hipError_t e = accumulate < 0 ? embed_launch(any, vocab, d, dtype, any, true, n, 1.0f, any, w_dtype, nullptr)
                                             : embed_backward_launch(any, dtype, any, true, n, vocab, d, 1.0f, accumulate, any, w_dtype, any, nullptr);
-        printf("%%s\n", e == hipSuccess ? "" : "error");
+        printf("%%lu%%s\n", (unsigned long)looks, e == hipSuccess ? "" : " error");
+        looks = 0;
     }
     return 0;
 }
@@ -155,12 +160,13 @@ def program(tmp_path_factory, name, text):
 
 @pytest.fixture(scope="module")
 def embed(tmp_path_factory):
-    """(n, vocab, d, dtype, w_dtype, accumulate; -1: the lookup) -> kernels by name, each followed by 1 where its divisions of indices are right."""
+    """(n, vocab, d, dtype, w_dtype, accumulate; -1: the lookup) -> kernels by name, each followed by 1 where its grid and its divisions of indices are right, and how often sorting
+    workgroups look at a token."""
     return program(tmp_path_factory, "embed", EMBED)
 
 
 def wrong(embed, calls):
-    return [(c, r) for c, r in zip(calls, embed(calls)) if "error" in r or any(ok != "1" for ok in r[1::2])]
+    return [(c, r) for c, r in zip(calls, embed(calls)) if "error" in r or any(ok != "1" for ok in r[1:-1:2])]
 
 
 def test_quotients_of_wide_rows(embed):
@@ -180,7 +186,17 @@ def test_quotients(embed):
 
 def test_one_launch_for_few_tokens(embed):
     for call in ((1440, 1000, 256, F32, F32, 0), (1440, 1000, 256, F32, F32, 1), (40, 5000, 1023, F16, F16, 1), (20, 1000, 8191, F16, F16, 1)):
-        assert embed([call])[0][::2] == ["small"], call
+        assert embed([call])[0][:-1:2] == ["small"], call
+
+
+def test_sorting_takes_a_bounded_time(embed):
+    """Up to 2^27 - 1 tokens and 2^31 - 2 ids: what all sorting workgroups look at is a few times the tokens for every 2^19 ids."""
+    calls = [(n, vocab, 1, F16, F16, how) for n in (1, 8192, 8193, 100_000, 1 << 20, 1 << 24, (1 << 24) + 1, (1 << 27) - 1) for vocab in (1, 50_001, 524_288, 524_289, 700_000, 10_000_000, 1 << 30, (1 << 31) - 2)
+             for how in (0, 1)]
+    assert wrong(embed, calls) == []
+    for call, r in zip(calls, embed(calls)):
+        n, vocab = call[:2]
+        assert int(r[-1]) <= max(4 * n * -(-vocab // 524_288), 49_152 * 1024 * -(-vocab // 524_288)), (call, r)
 
 
 @pytest.fixture(scope="module")
