@@ -194,3 +194,15 @@ def test_refusals():
                         (lambda: M.maxsim_norm_rope_backward(X, X, f, w, workspace=torch.empty(16, dtype=torch.uint8, device=DEV)), "scratch|workspace")):
         with pytest.raises(M.MaxSimError, match=match):
             call()
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("d,by,eps", [(512, 8e17, 1e-6), (340, 1e18, 1e-6), (64, 2.3e18, 1e-6), (512, 1e-18, 0.0), (64, 1e-18, 0.0), (2, 1.3e19, 0.0)])
+def test_the_ends_of_what_squares_can_hold(d, by, eps, interleaved):
+    """Rows whose squares add up to just less than fp32 holds, and to as little as it holds with all of its digits."""
+    sign = randn(6, 3, d, seed=51).sign()
+    X, dY = sign * by, randn(6, 3, d, seed=52)
+    X[1] *= 0.5 + 0.5 * torch.rand(3, d, generator=gen(53), device=DEV)
+    w = 1 + 0.1 * randn(d, seed=54)
+    assert d * by * by * (1 + d * 2.0 ** -24) < torch.finfo(torch.float32).max and (eps > 0 or 0.25 * by * by > 2.0 ** -126)
+    both(X, dY, freqs_of(d // 2 * 2), w, w, 2, torch.arange(6, device=DEV), dict(), interleaved, eps=eps)
