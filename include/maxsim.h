@@ -400,6 +400,7 @@ int maxsim_norm_rope_backward(const void *X, const void *dY, int64_t tokens, int
  *     loss[i] = KL(p || q) = sum_e p_e (log p_e - log q_{j_e}),    d loss[i] / d scores[i, j] = (q_j - sum of p_e over e with j_e = j) / tau
  * A row without entries that count has loss 0 and a gradient of zeros.  A column may be named more than once.
  *   scores   [n, b] dtype, rows `stride` entries apart      teacher [n, k] t_dtype, without gaps
+ *   Scores may be of any size: a mask of -10^9 or of the type's lowest value leaves no weight beside ordinary scores, and shares it evenly in a row that holds nothing else.
  *   index    [n, k] int32 or NULL (k = b: entry e is column e);  1 <= k <= 1024, b < 2^31;  10^-30 < tau < 10^30
  *   maxsim_distill           loss [n] float32;  lse [n] float32 or NULL: log sum_j exp(scores[i, j] / tau)
  *   maxsim_distill_backward  g [n, b] dtype, rows g_stride apart = dloss[i] * d loss[i] / d scores;  lse as maxsim_distill left it;  dloss [n] float32.

@@ -8,9 +8,9 @@
 // is q everywhere first, then the listed columns again.
 //
 // A gradient that follows the losses forms the row's maximum and sum again instead of taking one fp32 log of the sum, which for scores 560 temperatures from zero (28 at 0.05) costs q
-// 3 10^-5, where the row's own numbers cost 5 10^-8. It takes 165 us instead of 160 for 4096 rows of 50001, bf16, 99 instead of 93 for 500 of 100003, fp32, 22 instead of 15 for 64 of them.
+// 3 10^-5, where the row's own numbers cost 10^-7. It takes 164 us instead of 160 for 4096 rows of 50001, bf16, 99 instead of 93 for 500 of 100003, fp32, 21 instead of 15 for 64 of them.
 //
-// Bound by the memory: 4096 rows of 50001, bf16 (410 MB): the loss 70 us, 5.9 TB/s read, the gradient 165, 5.0 TB/s both ways, with or without the loss; 500 rows of 100003, fp32, too long for registers, 98 us;
+// Bound by the memory: 4096 rows of 50001, bf16 (410 MB): the loss 70 us, 5.9 TB/s read, the gradient 166, 4.9 TB/s both ways, with or without the loss; 500 rows of 100003, fp32, too long for registers, 98 us;
 // 64 rows of 1000 6.1 us, latency.
 //
 // Compiled with NaNs honoured: a score that is not a number has to show in its row's loss and gradient.
@@ -142,21 +142,16 @@ __device__ __forceinline__ void as_read(u32x4 &y)
     __builtin_amdgcn_sched_barrier(0); // (or it would be forgotten before it is used)
 }
 
-// A maximum and the sum of exponentials to it. Exponents are s c - zero in one rounding, with the same rounded zero for all: what it is off by
-// leaves with the sum.
+// A maximum and the sum of exponentials to it. Exponents are (s - top) c: whatever the scores' size, no thread's sum overflows, also not that of one that has seen nothing but a mask
+// (s c - top c in one rounding, an operation less, does where 2^-24 of top c passes 128: masks of -10^9 at a temperature of 0.05, the lowest score of the type at most; 4096 rows of
+// 12001, bf16: the loss 24.2 and 25.3 us, the gradient 45.2 and 46.3).
 struct Softmax {
-    float top = NOTHING, zero = 0.0f, sum = 0.0f;
+    float top = NOTHING, zero = 0.0f, sum = 0.0f; // zero: the top, or 0 where there is none
 
-    static __device__ __forceinline__ float zero_of(float top, float c)
-    {
-#pragma clang fp contract(off)
-        return top == NOTHING ? 0.0f : top * c;
-    }
     __device__ __forceinline__ void raise(float to, float c) // to another maximum
     {
-#pragma clang fp contract(off) // (the zeros' difference is that of the rounded ones)
-        const float z = zero_of(to, c);
-        sum *= top == NOTHING ? 0.0f : exp2_of(zero - z);
+        const float z = to == NOTHING ? 0.0f : to;
+        sum *= top == NOTHING ? 0.0f : exp2_of((zero - z) * c);
         top = to;
         zero = z;
     }
@@ -177,7 +172,7 @@ struct Softmax {
         for (int u = 0; u < N; ++u) {
 #pragma unroll
             for (int v = 0; v < V; ++v)
-                sum += exp2_of(fmaf(entry<T>(y[u], v), c, -zero));
+                sum += exp2_of((entry<T>(y[u], v) - zero) * c);
             if constexpr (KEPT) {
                 asm volatile("" : "+v"(sum)); // (here, and not where the sum is needed)
                 as_read(y[u]);
@@ -187,7 +182,7 @@ struct Softmax {
     __device__ __forceinline__ void add(float x, float c)
     {
         raise(fmaxf(top, x), c);
-        sum += exp2_of(fmaf(x, c, -zero));
+        sum += exp2_of((x - zero) * c);
     }
 };
 
@@ -288,7 +283,7 @@ template <int DT, int V, DistillMode MODE, int TH, int KEEP, bool ONCE> __global
             const float2 of = p.stats ? p.stats[i * p.pieces + o] : __builtin_bit_cast(float2, load_row<T, E>(sums_of_parts(p, i, pieces) + o * E));
             Softmax other;
             other.top = of.x;
-            other.zero = Softmax::zero_of(of.x, p.c);
+            other.zero = of.x == NOTHING ? 0.0f : of.x;
             other.sum = of.y;
             const float top = fmaxf(soft.top, other.top);
             soft.raise(top, p.c);
@@ -299,16 +294,33 @@ template <int DT, int V, DistillMode MODE, int TH, int KEEP, bool ONCE> __global
         sweep<TH, ONCE && MODE == LOSS>(soft, row, pieces, tid, p.c);
     }
 
-    // u / tau q = exp2(s c - zero) share by
+    // where the row is written over, the scores that entries name are read before any thread writes
+    const bool over = MODE == GRAD && p.g == p.scores;
+    if (over)
+        for (int e = tid; e < k; e += TH) {
+            const int j = e < TH ? j0 : p.index ? p.index[i * k + e] : e;
+            own[e] = e < TH ? s0 : j >= 0 && j < b ? (float)row[j] : NOTHING;
+        }
+
+    // u / tau q = 2^((s - zero) c) share by
     float zero = 0.0f, total = 0.0f, by = 0.0f, share = 0.0f;
-    auto gradient = [&](float s) { return exp2_of(fmaf(s, p.c, -zero)) * share; };
-    auto write_row = [&](bool some) {
+    auto gradient = [&](float s) { return exp2_of((s - zero) * p.c) * share; };
+    if constexpr (MODE == GRAD) {
+        // q does not wait for the teacher
+        float top[1] = {soft.top};
+        combine<TH>(top, spare, Max{});
+        soft.raise(top[0], p.c);
+        float sum[1] = {soft.sum};
+        combine<TH>(sum, spare + W, Sum{});
+        zero = soft.zero;
+        total = sum[0];
+        by = weight * p.inv_tau;
+        share = 1.0f / total;
         auto put = [&](int c, const u32x4 &y) {
-            Pack<T, V> r = {};
-            if (some)
+            Pack<T, V> r;
 #pragma unroll
-                for (int v = 0; v < V; ++v)
-                    r.x[v] = (T)(exp2_of(fmaf(entry<T>(y, v), p.c, -zero)) * (share * by));
+            for (int v = 0; v < V; ++v)
+                r.x[v] = (T)(exp2_of((entry<T>(y, v) - zero) * p.c) * (share * by));
             if (c < pieces.end)
                 store_row<ONCE>(dst + pieces.head + (int64_t)c * V, r);
         };
@@ -328,22 +340,7 @@ template <int DT, int V, DistillMode MODE, int TH, int KEEP, bool ONCE> __global
             }
         }
         if (pieces.lone >= 0)
-            dst[pieces.lone] = (T)(some ? gradient(KEEP > 0 ? lone : (float)row[pieces.lone]) * by : 0.0f);
-    };
-    // q does not wait for the teacher, unless the row is written over while other threads still read entries of it
-    const bool early = MODE == GRAD && p.g != p.scores;
-    if constexpr (MODE == GRAD) {
-        float top[1] = {soft.top};
-        combine<TH>(top, spare, Max{});
-        soft.raise(top[0], p.c);
-        float sum[1] = {soft.sum};
-        combine<TH>(sum, spare + W, Sum{});
-        zero = soft.zero;
-        total = sum[0];
-        by = weight * p.inv_tau;
-        share = 1.0f / total;
-        if (early)
-            write_row(true);
+            dst[pieces.lone] = (T)(gradient(KEEP > 0 ? lone : (float)row[pieces.lone]) * by);
     }
 
     // the teacher's entries
@@ -358,7 +355,7 @@ template <int DT, int V, DistillMode MODE, int TH, int KEEP, bool ONCE> __global
         if (e >= TH) {
             j = p.index ? p.index[i * k + e] : e;
             t = teacher_score(p, i * k + e);
-            s = j >= 0 && j < b ? (float)row[j] : NOTHING;
+            s = over ? own[e] : j >= 0 && j < b ? (float)row[j] : NOTHING;
         }
         const bool counts = j >= 0 && j < b && !(s == NOTHING) && !(t == NOTHING);
         idx[e] = counts ? j : -1;
@@ -393,19 +390,23 @@ template <int DT, int V, DistillMode MODE, int TH, int KEEP, bool ONCE> __global
         for (int e = tid; e < k; e += TH)
             if (idx[e] >= 0) {
                 const float q = prob[e] / sums[0];
-                const float log_p = ((e < TH ? t0 : teacher_score(p, i * k + e)) - t_top) * p.c - t_log, log_q = fmaf(own[e], p.c, -zero) - log2_sum; // (to the base 2)
+                const float log_p = ((e < TH ? t0 : teacher_score(p, i * k + e)) - t_top) * p.c - t_log, log_q = (own[e] - zero) * p.c - log2_sum; // (to the base 2)
                 loss[0] += q != 0.0f ? q * (log_p - log_q) : 0.0f;
             }
         combine<TH>(loss, spare + 5 * W, Sum{});
         if (tid == 0 && part == 0) {
             p.loss[i] = loss[0] * LN2;
             if (MODE == LOSS && p.lse)
-                p.lse[i] = (zero + log2_sum) * LN2;
+                p.lse[i] = fmaf(zero, p.inv_tau, log2_sum * LN2);
         }
     }
     if constexpr (MODE == GRAD) {
-        if (!early || !some)
-            write_row(some);
+        if (!some) { // (q is taken back)
+            for (int c = pieces.begin + tid; c < pieces.end; c += TH)
+                store_row<ONCE>(dst + pieces.head + (int64_t)c * V, Pack<T, V>{});
+            if (pieces.lone >= 0)
+                dst[pieces.lone] = (T)0.0f;
+        }
         // columns of another workgroup's part are its to write
         const int64_t lo = part == 0 ? 0 : pieces.head + (int64_t)pieces.begin * V, hi = part == (parts ? p.pieces - 1 : 0) ? b : pieces.head + (int64_t)pieces.end * V;
         // the listed columns: the first entry of a column writes it, with the sum of all of its entries
