@@ -406,7 +406,7 @@ int maxsim_norm_rope_backward(const void *X, const void *dY, int64_t tokens, int
  *   maxsim_distill_backward  g [n, b] dtype, rows g_stride apart = dloss[i] * d loss[i] / d scores;  lse as maxsim_distill left it;  dloss [n] float32.
  *                            The rows' sums are formed again, so that q is as exact as maxsim_distill_grad's (fp32's lse would cost it 2^-24 of lse's size)
  *   maxsim_distill_grad      both at once: g = weight * d loss[i] / d scores (weight: 1 / n for the mean, a loss scale);  loss [n] or NULL
- *   g may be scores itself, with its stride (and is otherwise apart from the inputs)
+ *   g may be scores itself, with its stride (and is otherwise apart from the inputs); then a row takes one workgroup: few rows of more than 128 KB are faster into another tensor
  *   workspace  maxsim_distill_workspace(n, b, dtype) bytes (device, 16-byte aligned; NULL where that is 0)
  * Everything is fp32, the gradient is rounded once.  The same bits on every run of tensors that lie alike (rows are taken in pieces of 16
  * aligned bytes: where a row begins in them shows in the last bits).  A NaN shows in its row's results.

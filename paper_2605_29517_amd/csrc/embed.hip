@@ -3,7 +3,7 @@
 // The lookup moves rows; a lane takes pieces of up to 32 bytes of any row. The gradient first sorts the token positions by id, in an order of the ids
 // that deals them to ranges in turn. Few tokens of little data: embed_small_kernel gives every workgroup a range, whose tokens it looks for among all, counts, lays down in order and
 // adds up. More of them: embed_scan_kernel does the same up to the sums, without a word from the other workgroups: where its first position belongs is the
-// number of tokens of the ranges before, which it has seen, too. Many tokens: embed_split_kernel sorts chunks of them by range, each within itself,
+// number of tokens of the ranges before, which it has seen, too. Many tokens, for 2^19 ids at a time: embed_split_kernel sorts chunks of them by range, each within itself,
 // and embed_place_kernel collects a range's parts from the chunks; where a range begins is the sum over the chunks of where it begins in them. Then a row of dW
 // is one sum over a run of the sorted positions. A run of more than `slice` positions is cut at multiples of it in the sorted order; the pieces' sums are joined in a
 // fixed order. No atomics on results: the same bits every time.

@@ -107,7 +107,9 @@ __device__ __forceinline__ float rows_sum(float x, int G)
     return x;
 }
 
-// N: pieces of a lane. A piece is two times V entries (the second V of a plain one are not there), or V with NEIGHBOURS.
+// N: pieces of a lane. A piece is two times V entries (the second V of a plain one are not there), or V with NEIGHBOURS. The gradient with HALVES and V = 8 is held to 128 registers, with
+// five of them in scratch (24 bytes a lane): 16384 tokens of 40 heads of 128 113 us, with 135 registers, three wavefronts to a SIMD and no scratch 117; 3850 tokens of 20 heads 29 and 33. All
+// gradients keep 41 to 101 scalars in lanes of a vector register.
 template <int DT, int V, NormPairs PAIRS, int N, bool BACK, bool ONCE> __global__ void __launch_bounds__(WG, N == 1 && BACK ? 4 : 1) norm_rope_kernel(NormParams p)
 {
     typedef typename Elem<DT>::T T;
@@ -353,7 +355,8 @@ __global__ void __launch_bounds__(WEIGHT_WG) norm_weight_kernel(NormParams p)
     }
 }
 
-// Runs of tokens in the gradient, each of which leaves two lines of dw: two to a slot of the chip or three (16384 tokens of 40 heads of 128: 113 us; 1280 runs 127, 4096 119)
+// Runs of tokens in the gradient, each of which leaves two lines of dw: two to each of the 1024 places for workgroups that the gradient with HALVES and V = 8 has (16384 tokens of 40 heads of
+// 128: 113 us; 1280 runs 127, 4096 119). That with NEIGHBOURS, of 91 registers, has 1280, which such a number fills one and a half times.
 constexpr int64_t MAX_RUNS = 2048;
 
 // How many tokens a workgroup takes
