@@ -219,3 +219,22 @@ def test_as_many_rows_as_there_are(distill, how):
             units = call[0] * (pieces if name == "stats" or how else 1)
             groups = -(-units // (x * y))  # of a workgroup, each with a row
             assert groups == 1 or threads // 64 >= groups, (call, name)
+
+
+def test_parts_of_a_row_hold_their_sums(distill):
+    """A gradient without a workspace passes every part's maximum and sum, 8 bytes, through the beginning of all parts of the row's gradient: the smallest part has room, wherever the row
+    begins in 16 bytes."""
+    calls = [(n, (32_768 * parts) // size + more, 1, dtype, 1, 2) for dtype, size in ((F32, 4), (F16, 2)) for n in (1, 2, 3, 7, 100, 255) for parts in (*range(1, 70), 127, 128, 511, 512, 513, 5000) for more in (0, 1, 8, 15)]
+    split = 0
+    for (n, b, _, dtype, *_), r in zip(calls, distill(calls)):
+        pieces, v = int(r[4]), 4 if dtype == F32 else 8
+        assert "error" not in r and pieces == int(r[-1])
+        if pieces > 1:
+            split += 1
+            for head in range(v):
+                every = (b - head) // v
+                each = -(-every // pieces)
+                assert 16 * (every - (pieces - 1) * each) >= 8 * pieces, (n, b, dtype, head)
+        else:
+            assert "stats" not in r
+    assert split > 100
